@@ -276,6 +276,150 @@ fgmp_status_t fgmp_quantize_weights_clip(const void *W, fgmp_dtype_t dt, int64_t
                                          void *stream);
 
 /*
+ * ---- Between the products of a layer: attention over a cache, the cache's upkeep, norms ----
+ *
+ * What a serving program runs between fgmp_quant_gemm_fused's products: fgmp_block_norm in front of and behind
+ * a block, fgmp_tree_attention for the tokens of a step (a single one, a chunk of a prompt, or a tree of drafted
+ * candidates), fgmp_cache_append for the tokens that are kept, and, for a cache held to a budget,
+ * fgmp_attention_weights and fgmp_cache_evict.  They follow the conventions above, but for what a cache's or a
+ * mask's unused places hold: that may be anything, NaN and infinities among it, and reaches no result.
+ * Non-finite values in places that are used give the results that IEEE arithmetic gives the formulas.
+ *
+ * A cache keeps `batch` sequences, each a row of slots; slot j of sequence b is row j % page_size of page
+ * page_table[b * table_stride + j / page_size], or row j of page b where page_table is null.  A slot holds one
+ * token's key and value for each of `heads` heads; element d of head h of row r of page p is at
+ * p * page_stride + r * token_stride + h * head_stride + d of `k` and of `v` alike (elements).  Attention
+ * does not depend on the order of the slots: keys come with their positions already applied.
+ *   lengths    device, one per sequence: slots in use, 0 .. the sequence's number of slots (clamped to that range)
+ *   page_table device; entries behind a sequence's last slot in use are not read.  An entry outside 0 .. pages - 1
+ *              is an error that is not reported: reads take page 0 instead, writes are dropped.  Sequences may share pages
+ *              that nothing is appended to and nothing evicted from.
+ *   page_size  a multiple of 16 with a page table, any number of slots without; head_dim 64, 128 or 256
+ * Pointers and strides are multiples of 16 bytes.  The struct itself is read during the call only.
+ */
+typedef struct {
+    void *k, *v;
+    fgmp_dtype_t dtype;
+    int32_t batch, heads, head_dim, page_size;
+    int32_t pages_per_sequence;   /* entries of a sequence's row of page_table; 1 without one */
+    int64_t pages;                /* pages that k and v hold */
+    int64_t page_stride, token_stride, head_stride;
+    const int32_t *page_table;
+    int64_t table_stride;
+    const int32_t *lengths;
+} fgmp_cache_t;
+
+/* Vectors of head_dim elements, contiguous, for each of batch x tokens x heads: where they lie (strides in elements).  A
+ * stride may be 0 in what is read, so that vectors are shared. */
+typedef struct {
+    void *data;
+    int64_t batch_stride, token_stride, head_stride;
+} fgmp_heads_t;
+
+/*
+ * Attention of `tokens` new tokens per sequence over the cache and over each other:
+ *   s_j = scale <q, k_j>;  out = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m);  lse = m + log sum_j e^(s_j - m),  m = max_j s_j
+ * with j over the slots in use and the new tokens that the token sees; q_heads / cache->heads consecutive query
+ * heads share a key head.  A token that sees nothing, or nothing but scores of -inf, gets out = 0
+ * and lse = -inf.
+ *   q, out     batch x tokens x q_heads vectors of the cache's dtype;  q_heads a multiple of cache->heads
+ *   k, v       the new tokens' keys and values, batch x tokens x cache->heads vectors of the cache's dtype (they are not
+ *              written to the cache); both nullable: the tokens attend to the cache alone
+ *   tree       nullable (a chain: token i sees the new tokens 0 .. i); batch x tokens rows of (tokens + 63) / 64
+ *              64-bit words, without padding, bit j of a row set if the token sees new token j (its own bit included, where it sees itself)
+ *   counts     nullable (all); per sequence, 0 .. tokens: new tokens from counts[b] on are seen by nobody, and get
+ *              out = 0, lse = -inf
+ *   max_length a hint: no smaller than the longest sequence, if the work is to be shared out well (results are right with any);
+ *              0: the number of slots
+ *   lse        batch x tokens x q_heads FP32
+ *   workspace  >= fgmp_tree_attention_workspace_bytes of the same sizes, with the same max_length or a larger one (the number of slots
+ *              where it is 0 here).  No control region is used: it need not be cleared.  May be null where that is 16 bytes.
+ * tokens <= 1024.  Sums and softmax statistics are FP32; with BF16 the weights e^(s_j - m) are rounded to BF16 for their product
+ * with v, and the sum that divides `out` is that of the rounded ones.
+ */
+size_t fgmp_tree_attention_workspace_bytes(int64_t batch, int64_t tokens, int64_t q_heads, int64_t heads, int64_t head_dim,
+                                           int64_t max_length);
+fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, const fgmp_heads_t *v, int64_t tokens,
+                                  int64_t q_heads, const fgmp_cache_t *cache, const uint64_t *tree, const int32_t *counts,
+                                  float scale, int64_t max_length, const fgmp_heads_t *out, float *lse, void *workspace,
+                                  size_t workspace_bytes, void *stream);
+
+/*
+ * The attention weight that accepted tokens give to each slot, added to what it had:
+ *   out[b, g, j] = weights[b, g, j] + sum_i sum_h e^(scale <q_ih, k_j> - lse_ih)
+ * over the accepted tokens i = 0 .. counts[b] - 1 of sequence b, which are its newest slots (call this after
+ * fgmp_cache_append), and the query heads h that share key head g; accepted token i sees the slots up to its own,
+ * j <= lengths[b] - counts[b] + i.
+ *   q, lse     as fgmp_tree_attention took and gave them, batch x tokens x q_heads
+ *   rows       nullable (token i is row i); batch x accepted: which of the `tokens` rows the i-th accepted token is; an
+ *              entry outside 0 .. tokens - 1 adds nothing
+ *   counts     nullable (accepted); per sequence, 0 .. accepted
+ *   weights, out  batch x cache->heads rows of `weights_stride` FP32 elements, one per slot; the same array, or arrays that do
+ *              not overlap.  Entries of slots not in use are neither read nor written.
+ */
+fgmp_status_t fgmp_attention_weights(const fgmp_heads_t *q, const float *lse, int64_t tokens, int64_t q_heads,
+                                     const fgmp_cache_t *cache, const int32_t *rows, int64_t accepted, const int32_t *counts,
+                                     float scale, int64_t max_length, const float *weights, float *out, int64_t weights_stride,
+                                     void *stream);
+
+/*
+ * Keys and values of accepted tokens into the cache: those of row rows[b, i] go to slot lengths[b] + i, i = 0 .. counts[b] - 1.
+ *   k, v       batch x tokens x cache->heads vectors of type `dt`, rounded to the cache's dtype where that is narrower
+ *   rows, accepted, counts  as above; an entry of `rows` outside 0 .. tokens - 1 leaves its slot as it is
+ *   positions  nullable; batch x tokens: a token's position in its sequence
+ *   slot_positions, slot_weights   nullable; batch x cache->heads rows of `slot_stride` elements: the new slots get
+ *              the token's position (needs `positions`) and weight 0
+ *   lengths_out  one per sequence: lengths[b] + counts[b]; an array of its own, not cache->lengths
+ * Tokens for which a sequence has no slots left are dropped.
+ */
+fgmp_status_t fgmp_cache_append(const fgmp_heads_t *k, const fgmp_heads_t *v, fgmp_dtype_t dt, int64_t tokens,
+                                const fgmp_cache_t *cache, const int32_t *rows, int64_t accepted, const int32_t *counts,
+                                const int32_t *positions, int32_t *slot_positions, float *slot_weights, int64_t slot_stride,
+                                int32_t *lengths_out, void *stream);
+
+/*
+ * A cache cut to `budget` slots per sequence, each head choosing for itself.  A sequence of more slots keeps `budget` of them:
+ * first those whose token is one of the first `sinks` (position < sinks) or of the newest `recent`
+ * (position >= seen[b] - recent), then those of the largest weight (NaN below all numbers; -0 and +0 alike); of equals, the
+ * lower slots.  What is kept of the slots from `budget` on moves, keys, values, weights and positions, into the slots below
+ * that were given up, both in ascending order; everything else stays in its place.
+ *   weights, positions   batch x cache->heads rows of `slot_stride` elements
+ *   seen       per sequence: tokens so far, the position of the next one
+ *   weights_out, positions_out   like them; entries below the new length are written, no others; each the same array as
+ *              its input, or one that overlaps nothing
+ *   lengths_out  min(lengths[b], budget); an array of its own, not cache->lengths
+ *   workspace  >= fgmp_cache_evict_workspace_bytes of the same sizes, slots = pages_per_sequence * page_size; need not be cleared
+ * budget >= 1; sinks, recent >= 0.
+ */
+size_t fgmp_cache_evict_workspace_bytes(int64_t batch, int64_t heads, int64_t slots, int64_t budget);
+fgmp_status_t fgmp_cache_evict(const fgmp_cache_t *cache, const float *weights, const int32_t *positions, int64_t slot_stride,
+                               const int32_t *seen, int64_t budget, int64_t sinks, int64_t recent, float *weights_out,
+                               int32_t *positions_out, int32_t *lengths_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The norms around a block, with its gate and residual scale:
+ *   y = residual_scale * x + branch_scale * act(gate) * N(o; post_weight, post_bias)
+ *   h = N(y; pre_weight, pre_bias)            with y before it is rounded to its dtype
+ *   N(z; w, b) = w * (z - mean) / sqrt(mean((z - mean)^2) + eps) + b;  FGMP_NORM_RMS: without the mean
+ * x is the residual stream, o what the block (the products between two norms) gave, h the next block's input.
+ *   o          nullable: the first norm of a model, y = x and is not written (`gate`, `post_*` and `y` must then be null)
+ *   post_weight, pre_weight   FP32, K values.  post_weight null: o is taken as it is (post_bias must be null);
+ *              pre_weight null: no h (the end of the last block; pre_bias and `h` must be null)
+ *   post_bias, pre_bias       nullable, FP32, K values
+ *   gate       nullable, dtype of o; row r of x uses gate row r / gate_rows: 1 for a gate of its own in every row,
+ *              M (or more) for one value per channel.  gate_act applies to its elements.
+ *   y          M x K, dtype of x, may be x itself;  h  M x K, dtype h_dt.  Leading dimensions in elements.
+ * K % 16 == 0, K <= 32768.  Every number is FP32 between the inputs and the one rounding of an output.
+ */
+typedef enum { FGMP_NORM_RMS = 0, FGMP_NORM_LAYER = 1 } fgmp_norm_t;
+typedef enum { FGMP_GATE_NONE = 0, FGMP_GATE_SIGMOID = 1, FGMP_GATE_SILU = 2 } fgmp_gate_t;
+fgmp_status_t fgmp_block_norm(const void *x, fgmp_dtype_t x_dt, int64_t ldx, const void *o, fgmp_dtype_t o_dt, int64_t ldo,
+                              const void *gate, int64_t ld_gate, int64_t gate_rows, fgmp_gate_t gate_act, int64_t M, int64_t K,
+                              const float *post_weight, const float *post_bias, const float *pre_weight, const float *pre_bias,
+                              fgmp_norm_t kind, float eps, float residual_scale, float branch_scale, void *y, int64_t ldy, void *h,
+                              fgmp_dtype_t h_dt, int64_t ldh, void *stream);
+
+/*
  * Expand a packed tensor to layout-independent arrays (for tests and tools):
  *   codes   rows*K bytes: E2M1 code 0..15 (FP4 block) or E4M3 byte (FP8 block)
  *   scales  rows*K/16 bytes: E4M3 block scale, 0 for FP8 blocks

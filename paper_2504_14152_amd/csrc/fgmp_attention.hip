@@ -1,0 +1,736 @@
+// Attention of new tokens over a cache and over each other.
+//
+// The query heads that share a key head, for all new tokens of a sequence, are the rows of one product with that head's keys:
+// row r = token * group + head of the group.  A wave holds 16 kRows of them in registers and walks over the keys in tiles, each
+// wave tiles of its own, with the running maximum and sum of the softmax (one pass over keys and values):
+//   S^T = K Q^T    a 16 x 16 tile of matrix instructions has keys along the registers and rows along the lanes, so that
+//   O^T += V^T P^T takes the weights P from the registers they were computed in, with no exchange between lanes: the order of the keys
+//                  in the k index of a matrix instruction is free, as long as both operands have the same.
+// Lane l = 16 g + i then holds, of the weights, row i and keys 4 g .. 4 g + 3 of each 16, and of V the same keys and the
+// elements d = n i .. n i + n - 1 (n = head_dim / 16): 16 lanes load a whole row of V, and BF16 values change places within the
+// lane's registers (32 v_perm for 8 keys x 8 elements).  K is loaded in operand order: 16 rows x 64 bytes an instruction.
+#include <algorithm>
+
+#include "fgmp_cache.hpp"
+
+namespace fgmp {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kWaves = 4;
+constexpr int kMaxTokens = 1024;
+
+struct AttendArgs {
+    CacheView c;
+    const char *q, *k, *v;
+    char *out;
+    float *lse;
+    int64_t q_batch, q_token, q_head, k_batch, k_token, k_head, v_batch, v_token, v_head, o_batch, o_token, o_head;   // bytes
+    const uint64_t *tree;
+    const int32_t *counts;
+    int32_t tokens, q_heads, group, words;
+    int32_t row_blocks, splits;      // workgroups per sequence and head: row blocks x ranges of keys
+    float c2;                        // scale * log2(e)
+    float *part_o, *part_ml;         // partial results of each range: [row][split][dim], [row][split][2]
+};
+
+template <bool kF32>
+struct Elem;
+template <>
+struct Elem<false> {
+    static constexpr int kSize = 2, kKeys = 32;   // keys of a tile: one matrix instruction's k index in the second product
+};
+template <>
+struct Elem<true> {
+    static constexpr int kSize = 4, kKeys = 16;
+};
+
+// Keys (or queries) of 16 rows as an operand: lane 16 g + i holds row i, and of every 64 bytes of it the g-th 16.
+template <bool kF32, int kDim>
+struct Operand {
+    static constexpr int kPieces = kDim * Elem<kF32>::kSize / 64;
+    u32x4 x[kPieces];
+    __device__ __forceinline__ void load(const char *row_and_lane)   // the lane's row + 16 g bytes
+    {
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) x[p] = *reinterpret_cast<const u32x4 *>(row_and_lane + 64 * p);
+    }
+};
+
+template <bool kF32, int kDim>
+__device__ __forceinline__ f32x4 scores(const Operand<kF32, kDim> &a, const Operand<kF32, kDim> &b)
+{
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int p = 0; p < Operand<kF32, kDim>::kPieces; ++p) {
+        if constexpr (kF32) {
+            const f32x4 x = __builtin_bit_cast(f32x4, a.x[p]), y = __builtin_bit_cast(f32x4, b.x[p]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], s, 0, 0, 0);
+        } else {
+            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.x[p]), __builtin_bit_cast(bf16x8, b.x[p]), s, 0, 0, 0);
+        }
+    }
+    return s;
+}
+
+// Values of a tile's keys: lane 16 g + i holds elements n i .. n i + n - 1 of its 4 (FP32) or 8 (BF16) keys.
+template <bool kF32, int kDim>
+struct Values {
+    static constexpr int kPer = kDim / 16, kLaneKeys = kF32 ? 4 : 8, kWords = kPer * Elem<kF32>::kSize / 4;
+    uint32_t x[kLaneKeys][kWords];
+    __device__ __forceinline__ void load(int key, const char *at)
+    {
+        if constexpr (kWords == 2) {
+            const u32x2 t = *reinterpret_cast<const u32x2 *>(at);
+            x[key][0] = t[0], x[key][1] = t[1];
+        } else {
+#pragma unroll
+            for (int p = 0; p < kWords / 4; ++p) {
+                const u32x4 t = *reinterpret_cast<const u32x4 *>(at + 16 * p);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[key][4 * p + e] = t[e];
+            }
+        }
+    }
+    __device__ __forceinline__ void clear(int key)
+    {
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) x[key][w] = 0u;
+    }
+    static __device__ __forceinline__ bool finite(uint32_t w)
+    {
+        return kF32 ? (w & 0x7F800000u) != 0x7F800000u : (w & 0x7F800000u) != 0x7F800000u && (w & 0x7F80u) != 0x7F80u;
+    }
+    __device__ __forceinline__ bool all_finite() const
+    {
+        bool fine = true;
+#pragma unroll
+        for (int j = 0; j < kLaneKeys; ++j)
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) fine = fine && finite(x[j][w]);
+        return fine;
+    }
+    // zeros in place of elements that are not finite
+    __device__ __forceinline__ void clear_non_finite()
+    {
+#pragma unroll
+        for (int j = 0; j < kLaneKeys; ++j)
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) {
+                const uint32_t t = x[j][w];
+                if constexpr (kF32) x[j][w] = finite(t) ? t : 0u;
+                else x[j][w] = ((t & 0x7F80u) != 0x7F80u ? t & 0xFFFFu : 0u) | ((t & 0x7F800000u) != 0x7F800000u ? t & 0xFFFF0000u : 0u);
+            }
+    }
+    // the m-th element of all the lane's keys, as the operand of the second product
+    __device__ __forceinline__ bf16x8 column(int m) const
+    {
+        u32x4 t;
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+            t[p] = __builtin_amdgcn_perm(x[2 * p + 1][m / 2], x[2 * p][m / 2], (m & 1) != 0 ? 0x07060302u : 0x05040100u);
+        return __builtin_bit_cast(bf16x8, t);
+    }
+};
+
+// Online softmax state and results of 16 rows: lane 16 g + i has row i; o[m][j] is element n (4 g + j) + m.
+template <int kDim>
+struct RowState {
+    float m, l, lr;   // maximum (of unscaled scores), sum of the weights (lane's keys only) and of the rounded ones
+    f32x4 o[kDim / 16];
+};
+
+__device__ __forceinline__ float over_groups_max(float x)
+{
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float over_groups_sum(float x)
+{
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+// One tile: s[sub][j] are the lane's scores (masked ones -inf), v the values.
+template <bool kF32, int kDim>
+__device__ __forceinline__ void absorb(RowState<kDim> &st, const f32x4 *s, const Values<kF32, kDim> &v, const bf16x8 *columns, float c2)
+{
+    constexpr int kSubs = kF32 ? 1 : 2, kPer = kDim / 16;
+    float most = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+    if constexpr (kSubs == 2) most = fmaxf(most, fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    most = fmaxf(over_groups_max(most), st.m);
+    if (__any(most > st.m)) {
+        // (-inf - -inf: nothing has been seen yet, whatever factor is applied to zeros)
+        const float alpha = st.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((st.m - most) * c2);
+        st.m = most;
+        st.l *= alpha;
+        st.lr *= alpha;
+#pragma unroll
+        for (int m = 0; m < kPer; ++m) st.o[m] *= alpha;
+    }
+    const float base = st.m == -INFINITY ? 0.0f : st.m * c2;
+    float p[4 * kSubs];
+#pragma unroll
+    for (int i = 0; i < 4 * kSubs; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], c2, -base));
+        st.l += p[i];
+    }
+    if constexpr (kF32) {
+#pragma unroll
+        for (int m = 0; m < kPer; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                st.o[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, v.x[j][m]), p[j], st.o[m], 0, 0, 0);
+    } else {
+        bf16x8 pb;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pb[i] = (__bf16)p[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) st.lr += (float)pb[i];
+#pragma unroll
+        for (int m = 0; m < kPer; ++m) st.o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(columns[m], pb, st.o[m], 0, 0, 0);
+    }
+}
+
+// What absorb() left out of a tile of new tokens: elements of V that are not finite, which rows that do not see their token must
+// not meet, not even with a weight of zero.  `v` points at the tile's first token.
+template <bool kF32, int kDim>
+__device__ __forceinline__ void add_non_finite(RowState<kDim> &st, const f32x4 *s, uint32_t sees, const char *v, int64_t v_token, int keys, float c2)
+{
+    constexpr int kPer = kDim / 16;
+    const int lane = threadIdx.x & 63, g = lane >> 4, i = lane & 15;
+    const float base = st.m == -INFINITY ? 0.0f : st.m * c2;
+    for (int key = 0; key < keys; ++key) {
+        const f32x4 mine = kF32 || key < 16 ? s[0] : s[1];
+        const float own = key % 4 == 0 ? mine[0] : key % 4 == 1 ? mine[1] : key % 4 == 2 ? mine[2] : mine[3];
+        float p = __builtin_amdgcn_exp2f(__builtin_fmaf(__shfl(own, key % 16 / 4 * 16 + i), c2, -base));
+        if (!kF32) p = (float)(__bf16)p;
+        if ((sees >> key & 1u) == 0u) continue;
+        const char *at = v + key * v_token;
+#pragma unroll
+        for (int m = 0; m < kPer; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int d = kPer * (4 * g + j) + m;
+                const float x = kF32 ? reinterpret_cast<const float *>(at)[d] : (float)reinterpret_cast<const __bf16 *>(at)[d];
+                if (!(fabsf(x) < INFINITY)) st.o[m][j] += p * x;
+            }
+    }
+}
+
+// kRows: groups of 16 rows that a workgroup's waves hold, every wave all of them.
+template <bool kF32, int kDim, int kRows>
+__global__ void __launch_bounds__(64 * kWaves) attend_kernel(AttendArgs a)
+{
+    constexpr int kSize = Elem<kF32>::kSize, kKeys = Elem<kF32>::kKeys, kSubs = kKeys / 16, kPer = kDim / 16;
+    constexpr int kLaneKeys = Values<kF32, kDim>::kLaneKeys;
+    __shared__ float merge_o[kWaves][kRows * kPer * 4 * 64];
+    __shared__ float merge_ml[kWaves][kRows][3][16];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g = lane >> 4, i = lane & 15;
+    // ranges of keys of one row block next to each other, then row blocks, heads, sequences
+    uint32_t id = blockIdx.x;
+    const int split = id % a.splits;
+    id /= a.splits;
+    const int block = id % a.row_blocks;
+    id /= a.row_blocks;
+    const int h = id % a.c.heads, b = id / a.c.heads;
+
+    const int32_t n = a.c.length(b);
+    int32_t count = a.counts != nullptr ? a.counts[b] : a.tokens;
+    count = count < 0 ? 0 : count > a.tokens ? a.tokens : count;
+    const int rows = a.tokens * a.group, first = block * (16 * kRows);
+    const bool empty = first >= count * a.group;         // no row of this block belongs to a token that counts
+    if (empty && a.splits > 1) return;                   // (written by the launch that joins the ranges)
+    const int drafted = a.k != nullptr ? count : 0;
+
+    // this workgroup's tiles: the sequence's are dealt out in equal ranges, the new tokens' go with the last one
+    const int cache_tiles = (n + kKeys - 1) / kKeys;
+    const int per = std::max(kWaves, (cache_tiles + a.splits - 1) / a.splits);
+    const int used = std::max(1, (cache_tiles + per - 1) / per);
+    if (split >= used) return;
+    const int end = std::min(cache_tiles, (split + 1) * per);
+    const int draft_tiles = split == used - 1 ? (drafted + kKeys - 1) / kKeys : 0;
+
+    int token[kRows];
+    Operand<kF32, kDim> q[kRows];
+    RowState<kDim> st[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int row = first + 16 * r + i, t = row / a.group;
+        token[r] = t < count ? t : -1;                   // (no row: sees nothing)
+        const int at = row < rows ? t : 0, head = h * a.group + (row < rows ? row - t * a.group : 0);
+        q[r].load(a.q + b * a.q_batch + at * a.q_token + head * a.q_head + 16 * g);
+        st[r].m = -INFINITY;
+        st[r].l = st[r].lr = 0.0f;
+#pragma unroll
+        for (int m = 0; m < kPer; ++m) st[r].o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    Operand<kF32, kDim> kt[kSubs];
+    Values<kF32, kDim> vt;
+    const int dv = i * kPer * kSize;
+    if (!empty) {
+        for (int tile = split * per + wave; tile < end; tile += kWaves) {
+#pragma unroll
+            for (int sub = 0; sub < kSubs; ++sub) {
+                // slots behind the last one in use: their group may have no page; rows are read as the last one in use
+                const int u = std::min(kSubs * tile + sub, (n - 1) / 16), last = std::min(15, n - 1 - 16 * u);
+                const int64_t at = a.c.group_offset(b, (uint32_t)u, h);
+                kt[sub].load(a.c.k + at + (int64_t)std::min(i, last) * a.c.token_stride + 16 * g);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    vt.load(4 * sub + j, a.c.v + at + (int64_t)std::min(4 * g + j, last) * a.c.token_stride + dv);
+            }
+            const int left = n - tile * kKeys;
+            if (left < kKeys) {
+                // what lies behind the sequence must not meet a weight of zero: it might not be finite
+#pragma unroll
+                for (int j = 0; j < kLaneKeys; ++j)
+                    if (16 * (j / 4) + 4 * g + j % 4 >= left) vt.clear(j);
+            }
+            bf16x8 columns[kPer];
+            if constexpr (!kF32) {
+#pragma unroll
+                for (int m = 0; m < kPer; ++m) columns[m] = vt.column(m);
+            }
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                f32x4 s[kSubs];
+#pragma unroll
+                for (int sub = 0; sub < kSubs; ++sub) {
+                    s[sub] = scores<kF32, kDim>(kt[sub], q[r]);
+                    if (left < kKeys) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (16 * sub + 4 * g + j >= left) s[sub][j] = -INFINITY;
+                    }
+                }
+                absorb<kF32, kDim>(st[r], s, vt, columns, a.c2);
+            }
+        }
+        for (int tile = wave; tile < draft_tiles; tile += kWaves) {
+            const int start = tile * kKeys, last = drafted - 1 - start;
+#pragma unroll
+            for (int sub = 0; sub < kSubs; ++sub) {
+                kt[sub].load(a.k + b * a.k_batch + (start + std::min(16 * sub + i, last)) * a.k_token + h * a.k_head + 16 * g);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    vt.load(4 * sub + j, a.v + b * a.v_batch + (start + std::min(16 * sub + 4 * g + j, last)) * a.v_token + h * a.v_head + dv);
+            }
+#pragma unroll
+            for (int j = 0; j < kLaneKeys; ++j)
+                if (16 * (j / 4) + 4 * g + j % 4 > last) vt.clear(j);
+            const bool finite = __all(vt.all_finite());
+            if (!finite) vt.clear_non_finite();
+            bf16x8 columns[kPer];
+            if constexpr (!kF32) {
+#pragma unroll
+                for (int m = 0; m < kPer; ++m) columns[m] = vt.column(m);
+            }
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                // bit j: the lane's row sees new token start + j
+                uint32_t sees = 0u;
+                if (token[r] >= 0) {
+                    if (a.tree != nullptr) {
+                        const uint64_t word = a.tree[((int64_t)b * a.tokens + token[r]) * a.words + (start >> 6)];
+                        sees = (uint32_t)(word >> (start & 63));
+                    } else {
+                        const int upto = token[r] - start;
+                        sees = upto >= 31 ? 0xFFFFFFFFu : upto < 0 ? 0u : (2u << upto) - 1u;
+                    }
+                    if (last < 31) sees &= (2u << last) - 1u;
+                }
+                f32x4 s[kSubs];
+#pragma unroll
+                for (int sub = 0; sub < kSubs; ++sub) {
+                    s[sub] = scores<kF32, kDim>(kt[sub], q[r]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if ((sees >> (16 * sub + 4 * g + j) & 1u) == 0u) s[sub][j] = -INFINITY;
+                }
+                absorb<kF32, kDim>(st[r], s, vt, columns, a.c2);
+                if (!finite)
+                    add_non_finite<kF32, kDim>(st[r], s, sees, a.v + b * a.v_batch + start * a.v_token + h * a.v_head, a.v_token,
+                                               std::min(kKeys, last + 1), a.c2);
+            }
+        }
+    }
+
+    // join the waves: every one holds all rows over keys of its own
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const float l = over_groups_sum(st[r].l), lr = kF32 ? l : over_groups_sum(st[r].lr);
+        if (g == 0) {
+            merge_ml[wave][r][0][i] = st[r].m;
+            merge_ml[wave][r][1][i] = l;
+            merge_ml[wave][r][2][i] = lr;
+        }
+#pragma unroll
+        for (int m = 0; m < kPer; ++m)
+            *reinterpret_cast<f32x4 *>(&merge_o[wave][((r * kPer + m) * 64 + lane) * 4]) = st[r].o[m];
+    }
+    __syncthreads();
+    // wave w adds up elements m = w, w + 4, ... of each lane's rows
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int row = first + 16 * r + i;
+        float most = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) most = fmaxf(most, merge_ml[w][r][0][i]);
+        float f[kWaves], l = 0.0f, lr = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float m = merge_ml[w][r][0][i];
+            f[w] = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - most) * a.c2);
+            l += merge_ml[w][r][1][i] * f[w];
+            lr += merge_ml[w][r][2][i] * f[w];
+        }
+        const int t = row / a.group, head = h * a.group + row - t * a.group;
+        const int64_t place = ((int64_t)b * a.tokens + t) * a.q_heads + head;   // (of rows that exist)
+        const float inverse = lr > 0.0f ? 1.0f / lr : lr == 0.0f ? 0.0f : lr;    // (NaN stays)
+#pragma unroll
+        for (int m4 = 0; m4 < kPer / kWaves; ++m4) {
+            const int m = wave * (kPer / kWaves) + m4;
+            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) o += *reinterpret_cast<const f32x4 *>(&merge_o[w][((r * kPer + m) * 64 + lane) * 4]) * f[w];
+            if (row < rows) {
+                if (a.splits > 1) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) a.part_o[(place * a.splits + split) * kDim + kPer * (4 * g + j) + m] = o[j];
+                } else {
+                    char *to = a.out + b * a.o_batch + t * a.o_token + head * a.o_head;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int d = kPer * (4 * g + j) + m;
+                        const float x = t < count ? o[j] * inverse : 0.0f;
+                        if constexpr (kF32) reinterpret_cast<float *>(to)[d] = x;
+                        else reinterpret_cast<__bf16 *>(to)[d] = (__bf16)x;
+                    }
+                }
+            }
+        }
+        if (wave == 0 && g == 0 && row < rows) {
+            if (a.splits > 1) {
+                float *ml = a.part_ml + (place * a.splits + split) * 4;
+                ml[0] = most;
+                ml[1] = l;
+                ml[2] = lr;
+            } else {
+                a.lse[place] = t >= count || l == 0.0f ? -INFINITY : (most * a.c2 + __builtin_amdgcn_logf(l)) * kLn2;
+            }
+        }
+    }
+}
+
+// Joins the ranges of keys: one wave per row.
+template <bool kF32, int kDim>
+__global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int64_t all_rows)
+{
+    constexpr int kKeys = Elem<kF32>::kKeys, kPer = kDim / 64;
+    const int lane = threadIdx.x & 63;
+    const int64_t place = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (place >= all_rows) return;
+    const int head = (int)(place % a.q_heads);
+    const int64_t bt = place / a.q_heads;
+    const int t = (int)(bt % a.tokens), b = (int)(bt / a.tokens);
+    int32_t count = a.counts != nullptr ? a.counts[b] : a.tokens;
+    const int cache_tiles = (a.c.length(b) + kKeys - 1) / kKeys;
+    const int per = std::max(kWaves, (cache_tiles + a.splits - 1) / a.splits);
+    const int used = t < count ? std::max(1, (cache_tiles + per - 1) / per) : 0;
+    const float *ml = a.part_ml + place * a.splits * 4, *po = a.part_o + place * a.splits * kDim + lane * kPer;
+    float most = -INFINITY;
+    for (int s = 0; s < used; ++s) most = fmaxf(most, ml[4 * s]);
+    float l = 0.0f, lr = 0.0f, o[kPer] = {};
+    for (int s = 0; s < used; ++s) {
+        const float m = ml[4 * s], f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - most) * a.c2);
+        l += ml[4 * s + 1] * f;
+        lr += ml[4 * s + 2] * f;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] += po[s * kDim + e] * f;
+    }
+    const float inverse = lr > 0.0f ? 1.0f / lr : lr == 0.0f ? 0.0f : lr;
+    char *to = a.out + b * a.o_batch + t * a.o_token + head * a.o_head;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        if constexpr (kF32) reinterpret_cast<float *>(to)[lane * kPer + e] = o[e] * inverse;
+        else reinterpret_cast<__bf16 *>(to)[lane * kPer + e] = (__bf16)(o[e] * inverse);
+    }
+    if (lane == 0) a.lse[place] = l == 0.0f ? -INFINITY : (most * a.c2 + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// ---- attention weights of accepted tokens ----
+//
+// The first product alone, S = Q K^T, with rows along the registers: the sum over rows is then within a lane, but for its last
+// step over the four lane groups.  A wave holds 16 kWeightKeys keys in registers and walks over the accepted rows, of which the workgroup
+// stages kStage at a time in LDS, in operand order.  No sum is shared between waves: the order of additions is fixed.
+
+constexpr int kWeightKeys = 2, kStage = 32;
+
+struct WeightArgs {
+    CacheView c;
+    const char *q;
+    const float *lse;
+    int64_t q_batch, q_token, q_head;   // bytes
+    const int32_t *rows, *counts;
+    int32_t tokens, accepted, q_heads, group, blocks;
+    float c2;
+    const float *weights;
+    float *out;
+    int64_t stride;
+};
+
+template <bool kF32, int kDim>
+__global__ void __launch_bounds__(64 * kWaves) weights_kernel(WeightArgs a)
+{
+    constexpr int kPieces = Operand<kF32, kDim>::kPieces, kBlock = 16 * kWeightKeys * kWaves;
+    __shared__ u32x4 stage[kStage / 16][kPieces][64];
+    __shared__ float stage_lse[kStage];   // log2 of the row's sum; +inf: a row that adds nothing
+    __shared__ int32_t stage_end[kStage]; // slots that the row sees
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tid = threadIdx.x;
+    const int g = lane >> 4, i = lane & 15;
+    uint32_t id = blockIdx.x;
+    const int block = id % a.blocks;
+    id /= a.blocks;
+    const int h = id % a.c.heads, b = id / a.c.heads;
+    const int32_t n = a.c.length(b);
+    int32_t count = a.counts != nullptr ? a.counts[b] : a.accepted;
+    count = count < 0 ? 0 : count > a.accepted ? a.accepted : count;
+    const int rows = count * a.group;
+    for (int first = block * kBlock; first < n; first += a.blocks * kBlock) {
+        const int mine = first + wave * 16 * kWeightKeys;
+        Operand<kF32, kDim> kt[kWeightKeys];
+#pragma unroll
+        for (int s = 0; s < kWeightKeys; ++s) {
+            const int u = std::min(mine / 16 + s, (n - 1) / 16), last = std::min(15, n - 1 - 16 * u);
+            kt[s].load(a.c.k + a.c.group_offset(b, (uint32_t)u, h) + (int64_t)std::min(i, last) * a.c.token_stride + 16 * g);
+        }
+        float sum[kWeightKeys] = {};
+        for (int start = 0; start < rows; start += kStage) {
+            __syncthreads();
+            for (int p = tid; p < kStage / 16 * kPieces * 64; p += 64 * kWaves) {
+                const int r = start + p / (kPieces * 64) * 16 + (p & 15);
+                u32x4 x = {0u, 0u, 0u, 0u};
+                if (r < rows) {
+                    const int t = r / a.group, row = a.rows != nullptr ? a.rows[b * (int64_t)a.accepted + t] : t;
+                    if ((uint32_t)row < (uint32_t)a.tokens)
+                        x = *reinterpret_cast<const u32x4 *>(a.q + b * a.q_batch + row * a.q_token + (h * a.group + r - t * a.group) * a.q_head +
+                                                             p / 64 % kPieces * 64 + (p / 16 & 3) * 16);
+                }
+                stage[p / (kPieces * 64)][p / 64 % kPieces][p & 63] = x;
+            }
+            if (tid < kStage) {
+                const int r = start + tid, t = r / a.group;
+                float lse = INFINITY;
+                if (r < rows) {
+                    const int row = a.rows != nullptr ? a.rows[b * (int64_t)a.accepted + t] : t;
+                    if ((uint32_t)row < (uint32_t)a.tokens) lse = a.lse[((int64_t)b * a.tokens + row) * a.q_heads + h * a.group + r - t * a.group] * kLog2e;
+                }
+                stage_lse[tid] = lse;
+                stage_end[tid] = n - count + t + 1;
+            }
+            __syncthreads();
+#pragma unroll 1
+            for (int r = 0; r < kStage / 16 && start + 16 * r < rows; ++r) {
+                Operand<kF32, kDim> q;
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p) q.x[p] = stage[r][p][lane];
+                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&stage_lse[16 * r + 4 * g]);
+                const int4 ends = *reinterpret_cast<const int4 *>(&stage_end[16 * r + 4 * g]);
+#pragma unroll
+                for (int s = 0; s < kWeightKeys; ++s) {
+                    const f32x4 x = scores<kF32, kDim>(q, kt[s]);
+                    const int slot = mine + 16 * s + i;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], a.c2, -lse[j]));
+                        sum[s] += slot < (j == 0 ? ends.x : j == 1 ? ends.y : j == 2 ? ends.z : ends.w) && lse[j] != INFINITY ? w : 0.0f;
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < kWeightKeys; ++s) {
+            const float total = over_groups_sum(sum[s]);
+            const int slot = mine + 16 * s + i;
+            if (g == 0 && slot < n) {
+                const int64_t at = ((int64_t)b * a.c.heads + h) * a.stride + slot;
+                a.out[at] = a.weights[at] + total;
+            }
+        }
+    }
+}
+
+// How a call is shared out: groups of 16 rows per workgroup, row blocks, ranges of keys.
+struct AttendPlan {
+    int row_groups;
+    int64_t row_blocks, splits;
+};
+
+AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t heads, int64_t head_dim, int64_t max_length)
+{
+    AttendPlan p;
+    const int64_t groups = (tokens * (q_heads / heads) + 15) / 16;
+    p.row_groups = 1;
+    (void)head_dim;
+    p.row_blocks = (groups + p.row_groups - 1) / p.row_groups;
+    const int64_t whole = batch * heads * p.row_blocks;
+    // at least 128 keys in a range, and about four workgroups for each compute unit
+    p.splits = std::max<int64_t>(1, std::min((max_length + 127) / 128, (1024 + whole - 1) / whole));
+    return p;
+}
+
+size_t attend_bytes(const AttendPlan &p, int64_t rows, int64_t head_dim)
+{
+    return p.splits > 1 ? (size_t)(rows * p.splits * (head_dim + 4) * 4) : 0;
+}
+
+template <bool kF32, int kDim>
+void attend_launch(const AttendArgs &a, const AttendPlan &p, hipStream_t st)
+{
+    const dim3 grid((unsigned)(a.c.batch * a.c.heads * p.row_blocks * p.splits));
+    attend_kernel<kF32, kDim, 1><<<grid, 64 * kWaves, 0, st>>>(a);
+    if (p.splits > 1) {
+        const int64_t rows = (int64_t)a.c.batch * a.tokens * a.q_heads;
+        join_kernel<kF32, kDim><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(a, rows);
+    }
+}
+
+}  // namespace
+
+}  // namespace fgmp
+
+using namespace fgmp;
+
+extern "C" {
+
+size_t fgmp_tree_attention_workspace_bytes(int64_t batch, int64_t tokens, int64_t q_heads, int64_t heads, int64_t head_dim, int64_t max_length)
+{
+    if (batch <= 0 || tokens <= 0 || tokens > kMaxTokens || heads <= 0 || q_heads <= 0 || q_heads % heads != 0 || batch > 65535 ||
+        q_heads > 65535 || max_length < 0 || max_length > (int64_t)1 << 30 || (head_dim != 64 && head_dim != 128 && head_dim != 256))
+        return 0;
+    return std::max<size_t>(16, attend_bytes(attend_plan(batch, tokens, q_heads, heads, head_dim, max_length), batch * tokens * q_heads, head_dim));
+}
+
+fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, const fgmp_heads_t *v, int64_t tokens, int64_t q_heads,
+                                  const fgmp_cache_t *cache, const uint64_t *tree, const int32_t *counts, float scale, int64_t max_length,
+                                  const fgmp_heads_t *out, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    AttendArgs a = {};
+    fgmp_status_t rc = check_cache(cache, &a.c);
+    if (rc != FGMP_OK) return rc;
+    if (tokens <= 0 || q_heads <= 0 || lse == nullptr || (k == nullptr) != (v == nullptr) || !(scale > 0.0f) || !(scale < INFINITY) || max_length < 0)
+        return FGMP_ERR_INVALID_ARG;
+    if (q_heads % a.c.heads != 0) return FGMP_ERR_BAD_SHAPE;
+    if (tokens > kMaxTokens || q_heads > 65535) return FGMP_ERR_UNSUPPORTED;
+    const int size = dtype_size(cache->dtype), dim = a.c.head_dim;
+    if ((rc = check_heads(q, a.c.batch, tokens, q_heads, dim, size, false)) != FGMP_OK) return rc;
+    if ((rc = check_heads(out, a.c.batch, tokens, q_heads, dim, size, true)) != FGMP_OK) return rc;
+    if (k != nullptr) {
+        if ((rc = check_heads(k, a.c.batch, tokens, a.c.heads, dim, size, false)) != FGMP_OK) return rc;
+        if ((rc = check_heads(v, a.c.batch, tokens, a.c.heads, dim, size, false)) != FGMP_OK) return rc;
+    }
+    if (max_length == 0 || max_length > a.c.slots) max_length = a.c.slots;
+    const AttendPlan p = attend_plan(a.c.batch, tokens, q_heads, a.c.heads, dim, max_length);
+    const int64_t rows = a.c.batch * tokens * q_heads;
+    const size_t need = attend_bytes(p, rows, dim);
+    if (need > 0) {
+        if (workspace == nullptr) return FGMP_ERR_INVALID_ARG;
+        if (!aligned16(workspace)) return FGMP_ERR_BAD_ALIGN;
+        if (workspace_bytes < need) return FGMP_ERR_BUFFER_TOO_SMALL;
+    }
+    if (a.c.batch * a.c.heads * p.row_blocks * p.splits >= (int64_t)1 << 31) return FGMP_ERR_UNSUPPORTED;
+    a.q = static_cast<const char *>(q->data);
+    a.q_batch = q->batch_stride * size, a.q_token = q->token_stride * size, a.q_head = q->head_stride * size;
+    a.out = static_cast<char *>(out->data);
+    a.o_batch = out->batch_stride * size, a.o_token = out->token_stride * size, a.o_head = out->head_stride * size;
+    if (k != nullptr) {
+        a.k = static_cast<const char *>(k->data);
+        a.k_batch = k->batch_stride * size, a.k_token = k->token_stride * size, a.k_head = k->head_stride * size;
+        a.v = static_cast<const char *>(v->data);
+        a.v_batch = v->batch_stride * size, a.v_token = v->token_stride * size, a.v_head = v->head_stride * size;
+    }
+    a.lse = lse;
+    a.tree = tree;
+    a.counts = counts;
+    a.tokens = (int32_t)tokens;
+    a.q_heads = (int32_t)q_heads;
+    a.group = (int32_t)(q_heads / a.c.heads);
+    a.words = (int32_t)((tokens + 63) / 64);
+    a.row_blocks = (int32_t)p.row_blocks;
+    a.splits = (int32_t)p.splits;
+    a.c2 = scale * kLog2e;
+    a.part_o = static_cast<float *>(workspace);
+    a.part_ml = a.part_o + rows * p.splits * dim;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (cache->dtype == FGMP_F32) {
+        if (dim == 64) attend_launch<true, 64>(a, p, st);
+        else if (dim == 128) attend_launch<true, 128>(a, p, st);
+        else attend_launch<true, 256>(a, p, st);
+    } else {
+        if (dim == 64) attend_launch<false, 64>(a, p, st);
+        else if (dim == 128) attend_launch<false, 128>(a, p, st);
+        else attend_launch<false, 256>(a, p, st);
+    }
+    return hipGetLastError() == hipSuccess ? FGMP_OK : FGMP_ERR_HIP;
+}
+
+fgmp_status_t fgmp_attention_weights(const fgmp_heads_t *q, const float *lse, int64_t tokens, int64_t q_heads, const fgmp_cache_t *cache,
+                                     const int32_t *rows, int64_t accepted, const int32_t *counts, float scale, int64_t max_length,
+                                     const float *weights, float *out, int64_t weights_stride, void *stream)
+{
+    WeightArgs a = {};
+    fgmp_status_t rc = check_cache(cache, &a.c);
+    if (rc != FGMP_OK) return rc;
+    if (tokens <= 0 || accepted <= 0 || q_heads <= 0 || lse == nullptr || weights == nullptr || out == nullptr || !(scale > 0.0f) ||
+        !(scale < INFINITY) || max_length < 0)
+        return FGMP_ERR_INVALID_ARG;
+    if (q_heads % a.c.heads != 0 || (rows == nullptr && accepted > tokens) || weights_stride < a.c.slots) return FGMP_ERR_BAD_SHAPE;
+    if (tokens > kMaxTokens || accepted > kMaxTokens || q_heads > 65535) return FGMP_ERR_UNSUPPORTED;
+    const int size = dtype_size(cache->dtype), dim = a.c.head_dim;
+    if ((rc = check_heads(q, a.c.batch, tokens, q_heads, dim, size, false)) != FGMP_OK) return rc;
+    if (max_length == 0 || max_length > a.c.slots) max_length = a.c.slots;
+    constexpr int kBlock = 16 * kWeightKeys * kWaves;
+    const int64_t pairs = (int64_t)a.c.batch * a.c.heads;
+    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>((max_length + kBlock - 1) / kBlock, ((int64_t)1 << 30) / pairs));
+    a.q = static_cast<const char *>(q->data);
+    a.q_batch = q->batch_stride * size, a.q_token = q->token_stride * size, a.q_head = q->head_stride * size;
+    a.lse = lse;
+    a.rows = rows;
+    a.counts = counts;
+    a.tokens = (int32_t)tokens;
+    a.accepted = (int32_t)accepted;
+    a.q_heads = (int32_t)q_heads;
+    a.group = (int32_t)(q_heads / a.c.heads);
+    a.blocks = (int32_t)blocks;
+    a.c2 = scale * kLog2e;
+    a.weights = weights;
+    a.out = out;
+    a.stride = weights_stride;
+    const dim3 grid((unsigned)(pairs * blocks));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (cache->dtype == FGMP_F32) {
+        if (dim == 64) weights_kernel<true, 64><<<grid, 64 * kWaves, 0, st>>>(a);
+        else if (dim == 128) weights_kernel<true, 128><<<grid, 64 * kWaves, 0, st>>>(a);
+        else weights_kernel<true, 256><<<grid, 64 * kWaves, 0, st>>>(a);
+    } else {
+        if (dim == 64) weights_kernel<false, 64><<<grid, 64 * kWaves, 0, st>>>(a);
+        else if (dim == 128) weights_kernel<false, 128><<<grid, 64 * kWaves, 0, st>>>(a);
+        else weights_kernel<false, 256><<<grid, 64 * kWaves, 0, st>>>(a);
+    }
+    return hipGetLastError() == hipSuccess ? FGMP_OK : FGMP_ERR_HIP;
+}
+
+}  // extern "C"

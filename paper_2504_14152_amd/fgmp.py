@@ -26,6 +26,19 @@ class FgmpError(RuntimeError):
     pass
 
 
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int), ("batch", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("pages_per_sequence", ctypes.c_int32), ("pages", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("page_table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("lengths", ctypes.c_void_p)]
+
+
+class _HeadsStruct(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
 class _PackedInfo(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("K", ctypes.c_int64), ("tensor_scale", ctypes.c_float),
                 ("compact", ctypes.c_int32), ("n_blocks", ctypes.c_int64),
@@ -157,6 +170,22 @@ def _load(path: str) -> ctypes.CDLL:
     L.fgmp_threshold_for_fraction_multi.restype = ctypes.c_int
     L.fgmp_threshold_for_fraction_multi.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.c_int32,
                                                     ctypes.c_double, ctypes.POINTER(f32), vp]
+    cache, heads = ctypes.POINTER(_CacheStruct), ctypes.POINTER(_HeadsStruct)
+    L.fgmp_tree_attention_workspace_bytes.restype = sz
+    L.fgmp_tree_attention_workspace_bytes.argtypes = [i64, i64, i64, i64, i64, i64]
+    L.fgmp_tree_attention.restype = ctypes.c_int
+    L.fgmp_tree_attention.argtypes = [heads, heads, heads, i64, i64, cache, vp, vp, f32, i64, heads, vp, vp, sz, vp]
+    L.fgmp_attention_weights.restype = ctypes.c_int
+    L.fgmp_attention_weights.argtypes = [heads, vp, i64, i64, cache, vp, i64, vp, f32, i64, vp, vp, i64, vp]
+    L.fgmp_cache_append.restype = ctypes.c_int
+    L.fgmp_cache_append.argtypes = [heads, heads, ctypes.c_int, i64, cache, vp, i64, vp, vp, vp, vp, i64, vp, vp]
+    L.fgmp_cache_evict_workspace_bytes.restype = sz
+    L.fgmp_cache_evict_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    L.fgmp_cache_evict.restype = ctypes.c_int
+    L.fgmp_cache_evict.argtypes = [cache, vp, vp, i64, vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]
+    L.fgmp_block_norm.restype = ctypes.c_int
+    L.fgmp_block_norm.argtypes = [vp, ctypes.c_int, i64, vp, ctypes.c_int, i64, vp, i64, i64, ctypes.c_int, i64, i64, vp, vp, vp, vp,
+                                  ctypes.c_int, f32, f32, f32, vp, i64, vp, ctypes.c_int, i64, vp]
     L.fgmp_selftest_encode_ranges.restype = ctypes.c_int
     L.fgmp_selftest_encode_ranges.argtypes = [ctypes.c_int, vp, vp, vp, vp]
     L.fgmp_selftest_decode_table.restype = ctypes.c_int
@@ -525,3 +554,236 @@ def selftest_decode_table(fmt: int, device="cuda"):
     out = torch.empty(256, dtype=torch.float32, device=device)
     _check(lib().fgmp_selftest_decode_table(fmt, _ptr(out), _stream()), "fgmp_selftest_decode_table")
     return out.cpu().numpy()
+
+
+# ---- between the products of a layer: attention over a cache, the cache's upkeep, norms ----
+
+class Cache:
+    """Keys and values of a batch of sequences (fgmp_cache_t): `k` and `v` pages x page_size x heads x head_dim, of the same type
+    and strides, head_dim contiguous; `page_table` batch x pages per sequence (int32), or None: sequence b's slots are page b;
+    `lengths` batch (int32), the slots in use.  The handle describes its tensors, checked once here; it allocates nothing
+    and nothing on the GPU is its own.  `lengths` may be exchanged for another tensor at any time (what cache_append and cache_evict return)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, lengths: torch.Tensor, page_table: torch.Tensor | None = None):
+        _require_cuda(k, v, lengths, page_table)
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(3) != 1:
+            raise FgmpError("k and v: the same pages x page_size x heads x head_dim, head_dim contiguous")
+        if page_table is not None:
+            _check_int32(page_table, "page_table")
+            if page_table.dim() != 2 or page_table.stride(1) != 1 or page_table.shape[0] != lengths.shape[0]:
+                raise FgmpError("page_table: batch x pages per sequence, rows contiguous")
+        self.k, self.v, self.page_table = k, v, page_table
+        pages, page_size, heads, dim = k.shape
+        self.batch, self.heads, self.head_dim, self.dtype = lengths.shape[0], heads, dim, k.dtype
+        per = 1 if page_table is None else page_table.shape[1]
+        self.slots = per * page_size
+        self._struct = _CacheStruct(k.data_ptr(), v.data_ptr(), _dtype_code(k), self.batch, heads, dim, page_size, per, pages,
+                                    k.stride(0), k.stride(1), k.stride(2), _ptr(page_table), 0 if page_table is None else page_table.stride(0),
+                                    None)
+        self._ref = ctypes.byref(self._struct)
+        self.lengths = lengths
+
+    @property
+    def lengths(self) -> torch.Tensor:
+        return self._lengths
+
+    @lengths.setter
+    def lengths(self, value: torch.Tensor) -> None:
+        _require_cuda(value)
+        _check_int32(value, "lengths", (self.batch,))
+        self._lengths = value
+        self._struct.lengths = value.data_ptr()
+
+
+def _check_int32(t: torch.Tensor | None, what: str, shape: tuple | None = None) -> None:
+    """int32 and, where a shape is asked for, contiguous of that shape."""
+    if t is not None and (t.dtype != torch.int32 or (shape is not None and (t.shape != shape or not t.is_contiguous()))):
+        raise FgmpError(f"{what}: int32" + ("" if shape is None else f", contiguous, of shape {tuple(shape)}"))
+
+
+def _check_f32(t: torch.Tensor | None, what: str, shape: tuple) -> None:
+    if t is not None and (t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous()):
+        raise FgmpError(f"{what}: float32, contiguous, of shape {tuple(shape)}")
+
+
+def _heads(t: torch.Tensor, what: str, shape: tuple, dtype: torch.dtype | None = None):
+    if t.shape != shape or t.stride(3) != 1 or (dtype is not None and t.dtype != dtype):
+        raise FgmpError(f"{what}: {'' if dtype is None else str(dtype) + ', '}of shape {tuple(shape)}, the last dimension contiguous")
+    s = t.stride()
+    return ctypes.byref(_HeadsStruct(t.data_ptr(), s[0], s[1], s[2]))
+
+
+def tree_words(parents) -> torch.Tensor:
+    """The `tree` of tree_attention (int64, on the CPU) for tokens whose parents are given, batch x tokens: the parent's index among
+    the new tokens, before the token's own, or -1 for one that follows the cache.  A token sees its ancestors and itself."""
+    parents = torch.as_tensor(parents).cpu().long()
+    B, T = parents.shape
+    if bool((parents >= torch.arange(T)).any()) or bool((parents < -1).any()):
+        raise FgmpError("a parent comes before its token, or is -1")
+    sees = torch.eye(T, dtype=torch.bool).repeat(B, 1, 1)
+    every = torch.arange(B)
+    for t in range(1, T):
+        p = parents[:, t]
+        sees[:, t] |= sees[every, p.clamp(min=0)] & (p >= 0)[:, None]
+    words = torch.zeros(B, T, -(-T // 64) * 64, dtype=torch.int64)
+    words[:, :, :T] = sees
+    return (words.view(B, T, -1, 64) << torch.arange(64)).sum(-1)
+
+
+def tree_attention_workspace_bytes(batch: int, tokens: int, q_heads: int, heads: int, head_dim: int, max_length: int) -> int:
+    return int(lib().fgmp_tree_attention_workspace_bytes(batch, tokens, q_heads, heads, head_dim, max_length))
+
+
+def tree_attention(q: torch.Tensor, k: torch.Tensor | None, v: torch.Tensor | None, cache: Cache, tree: torch.Tensor | None = None,
+                   counts: torch.Tensor | None = None, scale: float | None = None, max_length: int = 0, out: torch.Tensor | None = None,
+                   lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """(out, lse) of new tokens' attention over a cache and each other: q batch x tokens x query heads x head_dim; k, v batch x tokens x
+    heads x head_dim, or None.  `tree`: batch x tokens x words (int64, see tree_words), None for a chain; `counts` (int32): new tokens
+    of each sequence; `scale` 1 / sqrt(head_dim) unless given; `max_length`: the longest sequence, where the caller knows it."""
+    _require_cuda(q, k, v, tree, counts, out, lse, workspace)
+    if q.dim() != 4 or (k is None) != (v is None):
+        raise FgmpError("q: batch x tokens x heads x head_dim; k and v: both or neither")
+    B, T, H, D = q.shape
+    if B != cache.batch or D != cache.head_dim:
+        raise FgmpError("q does not match the cache")
+    dtype, new = cache.dtype, (B, T, cache.heads, D)
+    _check_int32(counts, "counts", (B,))
+    if tree is not None and (tree.dtype != torch.int64 or tree.shape != (B, T, (T + 63) // 64) or not tree.is_contiguous()):
+        raise FgmpError("tree: int64, contiguous, batch x tokens x (tokens + 63) // 64")
+    if out is None:
+        out = torch.empty((B, T, H, D), dtype=dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((B, T, H), dtype=torch.float32, device=q.device)
+    _check_f32(lse, "lse", (B, T, H))
+    if workspace is None:
+        workspace = torch.empty(tree_attention_workspace_bytes(B, T, H, cache.heads, D, max_length or cache.slots), dtype=torch.uint8,
+                                device=q.device)
+    rc = lib().fgmp_tree_attention(_heads(q, "q", (B, T, H, D), dtype), None if k is None else _heads(k, "k", new, dtype),
+                                   None if v is None else _heads(v, "v", new, dtype), T, H, cache._ref, _ptr(tree), _ptr(counts),
+                                   D ** -0.5 if scale is None else scale, max_length, _heads(out, "out", (B, T, H, D), dtype),
+                                   lse.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream())
+    _check(rc, "fgmp_tree_attention")
+    return out, lse
+
+
+def attention_weights(q: torch.Tensor, lse: torch.Tensor, cache: Cache, weights: torch.Tensor, rows: torch.Tensor | None = None,
+                      counts: torch.Tensor | None = None, scale: float | None = None, max_length: int = 0, out: torch.Tensor | None = None):
+    """`weights` (batch x heads x slots, float32) and what the accepted tokens' attention adds to it, in `out` (`weights` itself unless
+    given): call it after cache_append, with the q and lse that tree_attention took and gave.  `rows` (int32, batch x accepted): which
+    rows of q were accepted; `counts` (int32): how many of them."""
+    _require_cuda(q, lse, weights, rows, counts, out)
+    if q.dim() != 4 or q.shape[0] != cache.batch or q.shape[3] != cache.head_dim:
+        raise FgmpError("q does not match the cache")
+    B, T, H, D = q.shape
+    out = weights if out is None else out
+    accepted = _accepted(rows, counts, B, T)
+    _check_f32(lse, "lse", (B, T, H))
+    slots = (B, cache.heads, weights.shape[-1])
+    _check_f32(weights, "weights", slots)
+    _check_f32(out, "out", slots)
+    rc = lib().fgmp_attention_weights(_heads(q, "q", (B, T, H, D), cache.dtype), lse.data_ptr(), T, H, cache._ref, _ptr(rows), accepted,
+                                      _ptr(counts), D ** -0.5 if scale is None else scale, max_length, weights.data_ptr(),
+                                      out.data_ptr(), slots[2], _stream())
+    _check(rc, "fgmp_attention_weights")
+    return out
+
+
+def _accepted(rows: torch.Tensor | None, counts: torch.Tensor | None, B: int, T: int) -> int:
+    accepted = T if rows is None else rows.shape[-1]
+    _check_int32(rows, "rows", (B, accepted))
+    _check_int32(counts, "counts", (B,))
+    return accepted
+
+
+def cache_append(k: torch.Tensor, v: torch.Tensor, cache: Cache, rows: torch.Tensor | None = None, counts: torch.Tensor | None = None,
+                 positions: torch.Tensor | None = None, slot_positions: torch.Tensor | None = None,
+                 slot_weights: torch.Tensor | None = None, lengths_out: torch.Tensor | None = None) -> torch.Tensor:
+    """Keys and values of accepted tokens (`rows`, `counts` as attention_weights; k, v as tree_attention, float32 too) into the next slots
+    of the cache; returns the new lengths, for cache.lengths.  `positions` (int32, batch x tokens) go to `slot_positions` (int32, batch x
+    heads x slots); `slot_weights` (float32) of new slots become 0."""
+    _require_cuda(k, v, rows, counts, positions, slot_positions, slot_weights, lengths_out)
+    if k.dim() != 4 or k.dtype != v.dtype:
+        raise FgmpError("k and v: batch x tokens x heads x head_dim, of one type")
+    T = k.shape[1]
+    B, shape = cache.batch, (cache.batch, T, cache.heads, cache.head_dim)
+    accepted = _accepted(rows, counts, B, T)
+    _check_int32(positions, "positions", (B, T))
+    n = slot_weights.shape[-1] if slot_weights is not None else slot_positions.shape[-1] if slot_positions is not None else 0
+    _check_int32(slot_positions, "slot_positions", (B, cache.heads, n))
+    _check_f32(slot_weights, "slot_weights", (B, cache.heads, n))
+    if lengths_out is None:
+        lengths_out = torch.empty(B, dtype=torch.int32, device=k.device)
+    _check_int32(lengths_out, "lengths_out", (B,))
+    rc = lib().fgmp_cache_append(_heads(k, "k", shape), _heads(v, "v", shape), _dtype_code(k), T, cache._ref, _ptr(rows), accepted,
+                                 _ptr(counts), _ptr(positions), _ptr(slot_positions), _ptr(slot_weights), n, lengths_out.data_ptr(),
+                                 _stream())
+    _check(rc, "fgmp_cache_append")
+    return lengths_out
+
+
+def cache_evict_workspace_bytes(batch: int, heads: int, slots: int, budget: int) -> int:
+    return int(lib().fgmp_cache_evict_workspace_bytes(batch, heads, slots, budget))
+
+
+def cache_evict(cache: Cache, weights: torch.Tensor, positions: torch.Tensor, seen: torch.Tensor, budget: int, sinks: int = 0,
+                recent: int = 0, weights_out: torch.Tensor | None = None, positions_out: torch.Tensor | None = None,
+                lengths_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """Cuts every sequence to `budget` slots by accumulated attention weight (fgmp_cache_evict): keys and values move within the cache;
+    returns (weights, positions, lengths), the first two in place unless `weights_out` and `positions_out` are given."""
+    _require_cuda(weights, positions, seen, weights_out, positions_out, lengths_out, workspace)
+    weights_out = weights if weights_out is None else weights_out
+    positions_out = positions if positions_out is None else positions_out
+    shape = (cache.batch, cache.heads, weights.shape[-1])
+    _check_f32(weights, "weights", shape)
+    _check_f32(weights_out, "weights_out", shape)
+    _check_int32(positions, "positions", shape)
+    _check_int32(positions_out, "positions_out", shape)
+    _check_int32(seen, "seen", (cache.batch,))
+    if lengths_out is None:
+        lengths_out = torch.empty(cache.batch, dtype=torch.int32, device=weights.device)
+    _check_int32(lengths_out, "lengths_out", (cache.batch,))
+    if workspace is None:
+        workspace = torch.empty(max(16, cache_evict_workspace_bytes(cache.batch, cache.heads, cache.slots, budget)), dtype=torch.uint8,
+                                device=weights.device)
+    rc = lib().fgmp_cache_evict(cache._ref, weights.data_ptr(), positions.data_ptr(), shape[2], seen.data_ptr(), budget, sinks, recent,
+                                weights_out.data_ptr(), positions_out.data_ptr(), lengths_out.data_ptr(), workspace.data_ptr(),
+                                workspace.numel(), _stream())
+    _check(rc, "fgmp_cache_evict")
+    return weights_out, positions_out, lengths_out
+
+
+NORMS = {"rms": 0, "layer": 1}                          # fgmp_norm_t
+GATES = {"none": 0, "sigmoid": 1, "silu": 2}            # fgmp_gate_t
+
+
+def block_norm(x: torch.Tensor, o: torch.Tensor | None = None, post_weight: torch.Tensor | None = None,
+               post_bias: torch.Tensor | None = None, pre_weight: torch.Tensor | None = None, pre_bias: torch.Tensor | None = None,
+               gate: torch.Tensor | None = None, gate_act: str = "none", gate_rows: int = 0, kind: str = "rms", eps: float = 1e-5,
+               residual_scale: float = 1.0, branch_scale: float = 1.0, out: torch.Tensor | None = None, h: torch.Tensor | None = None,
+               h_dtype: torch.dtype | None = None):
+    """(y, h) of the norms around a block (fgmp_block_norm): y = residual_scale x + branch_scale act(gate) N(o; post), x itself where `o` is
+    None; h = N(y; pre), None without `pre_weight`.  x, o M x K; `gate` K values (one per channel) or rows of K, each for `gate_rows` rows of
+    x (1 unless given).  `out` (may be x) and `h` are made where they are not given, h in `h_dtype` or x's type."""
+    _require_cuda(x, o, post_weight, post_bias, pre_weight, pre_bias, gate, out, h)
+    M, K = x.shape
+    for t in (post_weight, post_bias, pre_weight, pre_bias):
+        _check_f32(t, "weights and biases", (K,))
+    if o is not None and out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    if pre_weight is not None and h is None:
+        h = torch.empty((M, K), dtype=h_dtype or x.dtype, device=x.device)
+    if gate is not None and gate.dim() == 1:
+        gate, gate_rows = gate[None], M
+    gate_rows = gate_rows or 1
+    for t, rows, dtype in ((x, M, None), (o, M, None), (out, M, x.dtype), (h, M, h_dtype), (gate, -(-M // gate_rows), o.dtype if o is not None else None)):
+        if t is not None and (t.dim() != 2 or t.shape[1] != K or t.shape[0] < rows or t.stride(1) != 1 or (dtype is not None and t.dtype != dtype)):
+            raise FgmpError("x, o, out, h: M x K, rows contiguous, out of x's type; gate: a row for each gate_rows rows of x, of o's type")
+    if kind not in NORMS or gate_act not in GATES:
+        raise FgmpError(f"kind: one of {sorted(NORMS)}; gate_act: one of {sorted(GATES)}")
+    rc = lib().fgmp_block_norm(x.data_ptr(), _dtype_code(x), x.stride(0), _ptr(o), 0 if o is None else _dtype_code(o),
+                               0 if o is None else o.stride(0), _ptr(gate), 0 if gate is None else gate.stride(0), gate_rows,
+                               GATES[gate_act], M, K, _ptr(post_weight), _ptr(post_bias), _ptr(pre_weight), _ptr(pre_bias), NORMS[kind],
+                               eps, residual_scale, branch_scale, _ptr(out), 0 if out is None else out.stride(0), _ptr(h),
+                               0 if h is None else _dtype_code(h), 0 if h is None else h.stride(0), _stream())
+    _check(rc, "fgmp_block_norm")
+    return (x if o is None else out), h

@@ -1,0 +1,694 @@
+"""What lies between a layer's products, on the GPU against its formulas in 64 bits: attention of new tokens over a cache, attention
+weights, upkeep of the cache, norms.
+
+Tolerances are bounds on rounding, element by element.  u is half an ulp: 2^-24 for FP32, 2^-8 for BF16.  A dot product of D terms is
+off by at most (D + 2) u times the sum of its terms' magnitudes; e^x by a relative |x| 2 u + 2 u; a weighted mean whose weights are off by
+a relative e by 2 e times the mean of magnitudes."""
+import math
+
+import pytest
+import torch
+
+from paper_2504_14152_amd import fgmp
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U32, U16 = 2.0 ** -24, 2.0 ** -8
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def _say(*what):
+    print(*what, flush=True)
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def _randn(g, *shape, dtype=F32):
+    return torch.randn(*shape, generator=g).to(dtype).to(DEV)
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _unit(dtype):
+    return U32 if dtype == F32 else U16
+
+
+def _poison(dtype, *shape):
+    """NaN and both infinities in turn."""
+    x = torch.tensor([math.nan, math.inf, -math.inf], dtype=dtype, device=DEV)
+    n = math.prod(shape)
+    return x.repeat(-(-n // 3))[:n].view(*shape)
+
+
+class Made:
+    """A cache of given lengths whose unused slots, pages and page table entries hold nothing fit for use."""
+
+    def __init__(self, g, lengths, heads, dim, page, dtype, room=0, order="slots"):
+        self.lens, B = list(lengths), len(lengths)
+        most = max(max(lengths) + room, 1)
+        each = -(-most // page) if page else 1
+        size = page or most + 5
+        pages = B * each + 2 if page else B
+        shape = (pages, size, heads, dim)
+        if order == "slots":
+            self.k, self.v = _poison(dtype, *shape), _poison(dtype, *shape)
+        else:   # heads outside of slots
+            self.k, self.v = (_poison(dtype, pages, heads, size, dim).transpose(1, 2) for _ in range(2))
+        self.table = None
+        if page:
+            self.table = torch.randperm(pages, generator=g)[: B * each].view(B, each).int()
+            self.used = self.table.clone()
+            for b, n in enumerate(lengths):
+                self.used[b, -(-(n + room) // page):] = -1 if b % 2 else 1 << 30
+        self.page, self.size, self.slots = page, size, size * each
+        self.keys, self.values = [], []
+        for b, n in enumerate(lengths):
+            k, v = _randn(g, n, heads, dim, dtype=dtype), _randn(g, n, heads, dim, dtype=dtype)
+            self.keys.append(k), self.values.append(v)
+            for j in range(0, n, size):
+                at = b if not page else int(self.table[b, j // size])
+                self.k[at, : min(size, n - j)] = k[j:j + size]
+                self.v[at, : min(size, n - j)] = v[j:j + size]
+        self.cache = fgmp.Cache(self.k, self.v, _i32(self.lens), None if not page else self.used.to(DEV))
+
+    def rows(self, pages, b, n):
+        """The first n slots of sequence b."""
+        if not self.page:
+            return pages[b, :n]
+        return torch.cat([pages[int(self.table[b, j // self.size])] for j in range(0, max(n, 1), self.size)])[:n]
+
+
+def _attention(q, keys, values, scale):
+    """softmax(scale q k) v in 64 bits, its logsumexp, bounds on |scores| sums and the mean of |v|: one query, one head."""
+    s = (keys.double() @ q.double()) * scale
+    lse = torch.logsumexp(s, 0)
+    w = torch.exp(s - lse)
+    size = float((keys.double().abs() @ q.double().abs()).max()) * scale
+    return (w[:, None] * values.double()).sum(0), float(lse), size, (w[:, None] * values.double().abs()).sum(0)
+
+
+def _compare_attention(out, lse, q, made, k, v, sees, counts, scale, group):
+    """`sees[b][t]`: new tokens that token t sees."""
+    B, T, H, D = q.shape
+    u = _unit(q.dtype)
+    out, lse = out.cpu().double(), lse.cpu().double()
+    q, k, v = q.cpu(), None if k is None else k.cpu(), None if v is None else v.cpu()
+    for b in range(B):
+        keys, values = made.keys[b].cpu(), made.values[b].cpu()
+        for t in range(T):
+            if t >= counts[b]:
+                assert bool((out[b, t] == 0).all()) and bool((lse[b, t] == -math.inf).all()), (b, t)
+                continue
+            new = [] if k is None else [j for j in sees[b][t] if j < counts[b]]
+            for h in range(H):
+                kh, vh = keys[:, h // group], values[:, h // group]
+                if new:
+                    kh, vh = torch.cat([kh, k[b, new, h // group]]), torch.cat([vh, v[b, new, h // group]])
+                if kh.shape[0] == 0:
+                    assert bool((out[b, t, h] == 0).all()) and lse[b, t, h] == -math.inf, (b, t, h)
+                    continue
+                want, want_lse, size, mean = _attention(q[b, t, h], kh, vh, scale)
+                n = kh.shape[0]
+                e_s = (D + 6) * U32 * size + 4 * U32 * (1 + abs(want_lse))
+                e_w = e_s + (n / 4 + 40) * U32
+                tol = (2 * e_w + (0.0 if u == U32 else 2.1 * U16)) * mean + u * want.abs() + 1e-30
+                assert bool(((out[b, t, h] - want).abs() <= tol).all()), (b, t, h, n, float(((out[b, t, h] - want).abs() / tol).max()))
+                assert abs(float(lse[b, t, h]) - want_lse) <= e_w + 4 * U32 * abs(want_lse), (b, t, h, n, float(lse[b, t, h]), want_lse)
+
+
+def _chain(B, T):
+    return [[list(range(t + 1)) for t in range(T)] for _ in range(B)]
+
+
+def _random_tree(g, B, T):
+    parents = torch.stack([torch.cat([torch.tensor([-1]), torch.stack([torch.randint(-1, t, (), generator=g) for t in range(1, T)])]) if T > 1
+                           else torch.tensor([-1]) for _ in range(B)])
+    sees = []
+    for b in range(B):
+        rows = []
+        for t in range(T):
+            up, p = [], t
+            while p >= 0:
+                up.append(p)
+                p = int(parents[b, p])
+            rows.append(sorted(up))
+        sees.append(rows)
+    return fgmp.tree_words(parents).to(DEV), sees
+
+
+ATTEND = [
+    # dtype, head_dim, query heads, heads, tokens, lengths, page, tree, counts
+    (BF16, 128, 4, 4, 1, [1], 0, False, None),
+    (BF16, 128, 8, 1, 1, [0, 31, 32, 33], 16, False, [1, 1, 1, 1]),
+    (BF16, 128, 8, 2, 3, [5, 0, 129, 640], 64, True, [3, 2, 0, 1]),
+    (BF16, 64, 6, 2, 17, [100, 47], 48, True, None),
+    (BF16, 64, 5, 1, 2, [15, 16, 17], 0, False, [2, 1, 2]),
+    (BF16, 256, 4, 2, 5, [333, 2], 32, True, [5, 4]),
+    (BF16, 128, 16, 2, 33, [1030, 64], 256, True, [33, 20]),
+    (BF16, 128, 2, 2, 65, [90], 16, True, None),
+    (BF16, 128, 3, 1, 130, [257], 64, False, [129]),
+    (F32, 64, 4, 4, 1, [1, 700], 0, False, None),
+    (F32, 128, 8, 2, 4, [0, 15, 16, 17], 16, True, [4, 4, 0, 3]),
+    (F32, 256, 2, 1, 7, [123], 48, True, None),
+    (F32, 64, 12, 2, 35, [515, 31], 64, True, [35, 17]),
+    (F32, 128, 1, 1, 67, [65], 0, False, None),
+]
+
+
+@pytest.mark.parametrize("dtype,D,H,G,T,lens,page,tree,counts", ATTEND)
+def test_attention_against_its_formula(dtype, D, H, G, T, lens, page, tree, counts):
+    _say("attention", dtype, D, H, G, T, lens, page, tree, counts)
+    g = _gen(D + T + H + len(lens))
+    B = len(lens)
+    made = Made(g, lens, G, D, page, dtype)
+    q, k, v = _randn(g, B, T, H, D, dtype=dtype), _randn(g, B, T, G, D, dtype=dtype), _randn(g, B, T, G, D, dtype=dtype)
+    q = q * 2
+    words, sees = _random_tree(g, B, T) if tree else (None, _chain(B, T))
+    use = [T] * B if counts is None else counts
+    for b in range(B):   # tokens that do not count are no numbers
+        k[b, use[b]:], v[b, use[b]:], q[b, use[b]:] = math.nan, math.inf, math.nan
+    scale = 1.0 / math.sqrt(D)
+    out, lse = fgmp.tree_attention(q, k, v, made.cache, tree=words, counts=None if counts is None else _i32(counts))
+    _compare_attention(out, lse, q, made, k, v, sees, use, scale, H // G)
+    # the cache alone, another scale
+    out, lse = fgmp.tree_attention(q, None, None, made.cache, counts=None if counts is None else _i32(counts), scale=0.37 * scale)
+    _compare_attention(out, lse, q, made, None, None, None, use, 0.37 * scale, H // G)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_hidden_tokens_reach_no_row_whatever_they_hold(dtype, bad):
+    """A new token whose key and value are not finite, seen by some rows and not by others: the others' results are as if it
+    were not there; those that see it get no finite result."""
+    g = _gen(3)
+    B, T, H, G, D = 1, 21, 4, 2, 64
+    made = Made(g, [77], G, D, 16, dtype)
+    q, k, v = _randn(g, B, T, H, D, dtype=dtype), _randn(g, B, T, G, D, dtype=dtype), _randn(g, B, T, G, D, dtype=dtype)
+    words, sees = _random_tree(g, B, T)
+    seen_by = [t for t in range(T) if 9 in sees[0][t]]
+    for which in ("v", "k", "both"):
+        _say("hidden tokens", dtype, bad, which)
+        kb, vb = k.clone(), v.clone()
+        if which != "v":
+            kb[0, 9] = bad
+        if which != "k":
+            vb[0, 9, :, ::3] = bad
+        out, lse = fgmp.tree_attention(q, kb, vb, made.cache, tree=words)
+        plain, plain_lse = fgmp.tree_attention(q, k, v, made.cache, tree=words)
+        for t in range(T):
+            if t in seen_by:
+                if which == "v":
+                    assert not bool(torch.isfinite(out[0, t, :, ::3]).any())
+                    assert torch.equal(out[0, t, :, 1::3], plain[0, t, :, 1::3]) and torch.equal(lse[0, t], plain_lse[0, t])
+            else:
+                assert torch.equal(out[0, t], plain[0, t]) and torch.equal(lse[0, t], plain_lse[0, t])
+
+
+def test_a_token_may_see_nothing_at_all():
+    g = _gen(4)
+    made = Made(g, [0, 3], 2, 128, 16, BF16)
+    q, k, v = _randn(g, 2, 4, 4, 128, dtype=BF16), _randn(g, 2, 4, 2, 128, dtype=BF16), _randn(g, 2, 4, 2, 128, dtype=BF16)
+    words = torch.zeros(2, 4, 1, dtype=torch.int64)
+    words[:, 2, 0] = 0b1000     # (a token need not see itself)
+    out, lse = fgmp.tree_attention(q, k, v, made.cache, tree=words.to(DEV))
+    sees = [[[], [], [3], []]] * 2
+    _compare_attention(out, lse, q, made, k, v, sees, [4, 4], 128 ** -0.5, 2)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attention_of_tensors_that_are_parts_of_others(dtype):
+    """Queries, keys and values as a fused product leaves them, a cache with its heads outside, results into a wider tensor, and one
+    token's vectors for all."""
+    g = _gen(5)
+    B, T, H, G, D = 3, 6, 8, 4, 64
+    made = Made(g, [50, 200, 17], G, D, 32, dtype, order="heads")
+    qkv = _randn(g, B, T, (H + 2 * G) * D, dtype=dtype)
+    q, k, v = (x.view(B, T, -1, D) for x in qkv.split([H * D, G * D, G * D], -1))
+    wide = torch.full((T, B, H, D + 32), 7.0, dtype=dtype, device=DEV)
+    out = wide[..., :D].transpose(0, 1)
+    _, lse = fgmp.tree_attention(q, k, v, made.cache, out=out)
+    _compare_attention(out, lse, q, made, k, v, _chain(B, T), [T] * B, D ** -0.5, H // G)
+    assert bool((wide[..., D:] == 7.0).all())
+    shared = k[:, :1].expand(B, T, G, D)
+    out, lse = fgmp.tree_attention(q, shared, shared, made.cache)
+    _compare_attention(out, lse, q, made, shared, shared, _chain(B, T), [T] * B, D ** -0.5, H // G)
+
+
+@pytest.mark.parametrize("dtype,H,T", [(BF16, 8, 1), (BF16, 16, 9), (F32, 8, 2), (BF16, 2, 64)])
+def test_ranges_of_a_long_cache_join(dtype, H, T):
+    """Lengths around every way to share a sequence out, and hints that are too small."""
+    g = _gen(6)
+    D, G = 128, 1
+    for n in (127, 128, 129, 1000, 4097, 20011):
+        made = Made(g, [n], G, D, 64, dtype, room=0)
+        q, k, v = _randn(g, 1, T, H, D, dtype=dtype) * 3, _randn(g, 1, T, G, D, dtype=dtype), _randn(g, 1, T, G, D, dtype=dtype)
+        for hint in (0, 1, 300):
+            out, lse = fgmp.tree_attention(q, k, v, made.cache, max_length=hint)
+            rows = sorted({0, T // 2, T - 1})
+            part = [list(range(t + 1)) for t in rows]
+            for t, new in zip(rows, part):
+                for h in (0, H - 1):
+                    kh = torch.cat([made.keys[0][:, 0], k[0, new, 0]]).cpu()
+                    vh = torch.cat([made.values[0][:, 0], v[0, new, 0]]).cpu()
+                    want, want_lse, size, mean = _attention(q[0, t, h].cpu(), kh, vh, D ** -0.5)
+                    e_w = (D + 6) * U32 * size + 4 * U32 * (1 + abs(want_lse)) + (n / 4 + 40) * U32
+                    tol = (2 * e_w + (0.0 if dtype == F32 else 2.1 * U16)) * mean + _unit(dtype) * want.abs()
+                    got = out[0, t, h].cpu().double()
+                    assert bool(((got - want).abs() <= tol).all()), (n, hint, t, h)
+                    assert abs(float(lse[0, t, h]) - want_lse) <= e_w + 4 * U32 * abs(want_lse)
+            again, lse2 = fgmp.tree_attention(q, k, v, made.cache, max_length=hint)
+            assert torch.equal(out, again) and torch.equal(lse, lse2)
+    _say("ranges", dtype, H, T)
+
+
+def test_offsets_past_32_bits():
+    """Pages and rows that lie more than 4 GiB behind their pointer."""
+    g = _gen(7)
+    D, G, page = 128, 2, 64
+    for dtype in (BF16, F32):
+        pages = (5 << 30) // (page * G * D * dtype.itemsize)
+        k, v = (torch.empty(pages, page, G, D, dtype=dtype, device=DEV) for _ in range(2))
+        table = [pages - 1, 0, pages - 7]
+        made = Made(g, [150], G, D, 0, dtype)
+        for j, at in enumerate(table):
+            m = min(page, 150 - page * j)
+            k[at, :m], v[at, :m] = made.keys[0][page * j:page * j + m], made.values[0][page * j:page * j + m]
+        cache = fgmp.Cache(k, v, _i32([150]), _i32([table]))
+        q = _randn(g, 1, 2, 4, D, dtype=dtype)
+        out, lse = fgmp.tree_attention(q, None, None, cache)
+        _compare_attention(out, lse, q, made, None, None, None, [2, 2], D ** -0.5, 2)
+        # one page of slots that far: rows apart by a wide stride
+        step = 1 << 24
+        long_k = torch.empty((150 * step + 256,), dtype=dtype, device=DEV)
+        rows = torch.as_strided(long_k, (1, 150, G, D), (150 * step, step, D, 1))
+        rows[0] = made.keys[0]
+        cache = fgmp.Cache(rows, rows, _i32([150]))
+        made.values[0] = made.keys[0]
+        out, lse = fgmp.tree_attention(q, None, None, cache)
+        _compare_attention(out, lse, q, made, None, None, None, [2, 2], D ** -0.5, 2)
+        w = fgmp.attention_weights(q, lse, cache, torch.zeros(1, G, 150, device=DEV), counts=_i32([1]))
+        assert bool(torch.isfinite(w).all())
+        _say("offsets", dtype)
+
+
+# ---- attention weights ----
+
+WEIGHTS = [
+    # dtype, head_dim, query heads, heads, tokens, lengths, page, accepted, counts
+    (BF16, 128, 4, 4, 1, [1], 0, 1, None),
+    (BF16, 128, 8, 1, 3, [3, 130, 64], 16, 2, [2, 1, 0]),
+    (BF16, 64, 6, 2, 17, [100, 17], 48, 17, None),
+    (BF16, 256, 4, 2, 5, [333, 2], 32, 3, [3, 2]),
+    (BF16, 128, 16, 2, 40, [1030, 257], 64, 40, [40, 35]),
+    (F32, 64, 4, 4, 1, [1, 700], 0, 1, None),
+    (F32, 128, 8, 2, 4, [4, 15, 16, 17], 16, 4, [4, 3, 0, 3]),
+    (F32, 256, 2, 1, 7, [123], 48, 5, None),
+]
+
+
+def _compare_weights(got, have, made, q, lse, rows, counts, scale, group):
+    got, have, q, lse = got.cpu().double(), have.cpu().double(), q.cpu().double(), lse.cpu().double()
+    for b, n in enumerate(made.lens):
+        keys = made.keys[b].cpu().double()
+        for h in range(keys.shape[1]):
+            want, tol = have[b, h, :n].clone(), U32 * 4 * have[b, h, :n].abs()
+            for i in range(counts[b]):
+                row = rows[b][i]
+                if not 0 <= row < q.shape[1]:
+                    continue
+                end = n - counts[b] + i + 1
+                for e in range(group):
+                    x = keys[:end, h] @ q[b, row, h * group + e] * scale
+                    size = keys[:end, h].abs() @ q[b, row, h * group + e].abs() * scale
+                    p = torch.exp(x - lse[b, row, h * group + e])
+                    want[:end] += p
+                    rel = (q.shape[3] + 6) * U32 * size + 4 * U32 * (2 + x.abs() + abs(float(lse[b, row, h * group + e])))
+                    tol[:end] += p * (rel + (counts[b] * group + 8) * U32)
+            err = (got[b, h, :n] - want).abs()
+            assert bool((err <= tol + 1e-30).all()), (b, h, float((err / (tol + 1e-30)).max()))
+
+
+@pytest.mark.parametrize("dtype,D,H,G,T,lens,page,accepted,counts", WEIGHTS)
+def test_attention_weights_against_their_formula(dtype, D, H, G, T, lens, page, accepted, counts):
+    _say("weights", dtype, D, H, G, T, lens, page, accepted, counts)
+    g = _gen(D + T + H)
+    B = len(lens)
+    made = Made(g, lens, G, D, page, dtype)
+    q = _randn(g, B, T, H, D, dtype=dtype) * 2
+    use = [accepted] * B if counts is None else counts
+    rows = [torch.randperm(T, generator=g)[:accepted].tolist() for _ in range(B)]
+    if accepted > 2:
+        rows[0][1] = T          # no such row: adds nothing
+        rows[-1][2] = -1
+    # sums that belong to the scores, as attention gives them
+    lse = torch.full((B, T, H), math.nan, device=DEV)
+    for b in range(B):
+        for i in range(use[b]):
+            if 0 <= rows[b][i] < T:
+                end = lens[b] - use[b] + i + 1
+                for h in range(H):
+                    s = made.keys[b][:end, h // (H // G)].double() @ q[b, rows[b][i], h].double() * D ** -0.5
+                    lse[b, rows[b][i], h] = torch.logsumexp(s, 0)
+    have = torch.full((B, G, made.slots + 3), math.nan, device=DEV)
+    for b, n in enumerate(lens):
+        have[b, :, :n] = _randn(g, G, n).abs()
+    out = torch.full_like(have, 5.0)
+    got = fgmp.attention_weights(q, lse, made.cache, have, rows=_i32(rows), counts=None if counts is None else _i32(counts), out=out)
+    assert got is out
+    _compare_weights(got, have, made, q, lse, rows, use, D ** -0.5, H // G)
+    for b, n in enumerate(lens):
+        assert bool((out[b, :, n:] == 5.0).all())
+    again = have.clone()
+    fgmp.attention_weights(q, lse, made.cache, again, rows=_i32(rows), counts=None if counts is None else _i32(counts), max_length=1)
+    for b, n in enumerate(lens):
+        assert torch.equal(again[b, :, :n], out[b, :, :n]) and bool(torch.isnan(again[b, :, n:]).all())
+
+
+def test_weights_of_a_whole_prompt_without_rows():
+    """Attention's own sums, every token accepted: each token's weights add up to one for every query head."""
+    g = _gen(9)
+    B, T, H, G, D = 2, 50, 4, 2, 64
+    made = Made(g, [0, 7], G, D, 16, BF16, room=T)
+    q, k, v = _randn(g, B, T, H, D, dtype=BF16), _randn(g, B, T, G, D, dtype=BF16), _randn(g, B, T, G, D, dtype=BF16)
+    _, lse = fgmp.tree_attention(q, k, v, made.cache)
+    made.cache.lengths = fgmp.cache_append(k, v, made.cache)
+    assert made.cache.lengths.tolist() == [50, 57]
+    w = fgmp.attention_weights(q, lse, made.cache, torch.zeros(B, G, made.slots, device=DEV))
+    for b, n in enumerate([50, 57]):
+        # (each of T * H / G sums of one is off by what lse and the exponentials are)
+        assert bool(((w[b, :, :n].double().sum(-1) - T * H / G).abs() < T * H / G * 1e-5).all())
+
+
+# ---- append ----
+
+@pytest.mark.parametrize("source", [BF16, F32])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("G,D,page,T,lens,counts", [(2, 64, 16, 5, [0, 15, 30], [5, 3, 0]), (8, 128, 0, 1, [9], None), (3, 256, 48, 9, [47, 48], [1, 9])])
+def test_append(source, dtype, G, D, page, T, lens, counts):
+    _say("append", source, dtype, G, D, page, T, lens, counts)
+    g = _gen(T + D)
+    B = len(lens)
+    made = Made(g, lens, G, D, page, dtype, room=T)
+    k, v = _randn(g, B, T, 2 * G, D, dtype=source)[:, :, ::2], _randn(g, B, T, G, D, dtype=source)
+    rows = torch.stack([torch.randperm(T, generator=g) for _ in range(B)]).int()
+    if T > 4:
+        rows[0, 1], rows[0, 2] = T, -3      # no such rows: their slots stay as they are
+    positions = torch.randint(0, 1000, (B, T), generator=g).int()
+    slot_positions = torch.full((B, G, made.slots), -7, dtype=torch.int32, device=DEV)
+    slot_weights = torch.full((B, G, made.slots), 3.0, device=DEV)
+    before_k, before_v = made.k.clone(), made.v.clone()
+    lengths = fgmp.cache_append(k, v, made.cache, rows=rows.to(DEV), counts=None if counts is None else _i32(counts), positions=positions.to(DEV),
+                                slot_positions=slot_positions, slot_weights=slot_weights)
+    use = [T] * B if counts is None else counts
+    want_k, want_v = before_k, before_v
+    want_p, want_w = torch.full_like(slot_positions, -7), torch.full_like(slot_weights, 3.0)
+    for b in range(B):
+        for i in range(use[b]):
+            r, slot = int(rows[b, i]), lens[b] + i
+            if 0 <= r < T:
+                at = b if not page else int(made.table[b, slot // page])
+                want_k[at, slot % made.size], want_v[at, slot % made.size] = k[b, r].to(dtype), v[b, r].to(dtype)
+                want_p[b, :, slot], want_w[b, :, slot] = int(positions[b, r]), 0.0
+    bits = torch.int16 if dtype == BF16 else torch.int32
+    assert torch.equal(made.k.view(bits), want_k.view(bits)) and torch.equal(made.v.view(bits), want_v.view(bits))
+    assert torch.equal(slot_positions, want_p) and torch.equal(slot_weights, want_w)
+    assert lengths.tolist() == [n + c for n, c in zip(lens, use)]
+
+
+def test_append_drops_what_has_no_slot():
+    g = _gen(10)
+    made = Made(g, [30, 32], 1, 64, 16, BF16)       # 32 slots each
+    before = made.v.clone()
+    k = _randn(g, 2, 4, 1, 64, dtype=BF16)
+    lengths = fgmp.cache_append(k, k, made.cache)
+    assert lengths.tolist() == [32, 32]
+    changed = (made.v.view(torch.int16) != before.view(torch.int16)).flatten(1).any(-1).nonzero().flatten().tolist()
+    assert changed == [int(made.table[0, 1])]
+    assert torch.equal(made.rows(made.v, 0, 32)[30:], k[0, :2])
+
+
+def test_a_page_that_is_none_of_the_cache_is_not_written():
+    g = _gen(11)
+    made = Made(g, [16], 1, 64, 16, BF16)
+    table = made.table.clone()
+    table = torch.cat([table, torch.tensor([[1 << 20]], dtype=torch.int32)], 1)
+    cache = fgmp.Cache(made.k, made.v, _i32([16]), table.to(DEV))
+    before = made.k.clone(), made.v.clone()
+    k = _randn(g, 1, 2, 1, 64, dtype=BF16)
+    assert fgmp.cache_append(k, k, cache).tolist() == [18]
+    assert torch.equal(made.k.view(torch.int16), before[0].view(torch.int16)) and torch.equal(made.v.view(torch.int16), before[1].view(torch.int16))
+
+
+# ---- evict ----
+
+def _evicted(w, p, n, seen, budget, sinks, recent):
+    """What each of the first min(n, budget) slots holds afterwards, by the definition."""
+    keep = min(n, budget)
+    if n <= budget:
+        return list(range(n))
+    fixed = [i for i in range(n) if p[i] < sinks or p[i] >= seen - recent]
+    inside = set(fixed)
+    others = sorted((i for i in range(n) if i not in inside), key=lambda i: (1, 0.0) if math.isnan(w[i]) else (0, -w[i]))
+    stay = set((fixed + others)[:budget])
+    now = list(range(keep))
+    movers = sorted(i for i in stay if i >= keep)
+    for hole, mover in zip([i for i in range(keep) if i not in stay], movers):
+        now[hole] = mover
+    return now
+
+
+EVICT = [
+    # heads, head_dim, page, dtype, lengths, budget, sinks, recent, values of the weights
+    (2, 64, 16, BF16, [40, 20, 21], 20, 2, 5, "random"),
+    (1, 128, 0, BF16, [1, 2, 0], 1, 0, 0, "random"),
+    (3, 128, 48, F32, [500, 499], 130, 4, 0, "ties"),
+    (2, 256, 32, BF16, [1100, 1024, 1025], 1024, 16, 64, "random"),
+    (1, 64, 16, BF16, [100], 30, 20, 40, "random"),         # more is fixed than there is room for
+    (2, 64, 64, F32, [3000], 2000, 4, 100, "special"),
+    (1, 64, 256, BF16, [70001], 1001, 0, 10, "random"),
+    (2, 64, 16, BF16, [64], 64, 0, 0, "random"),
+    (1, 64, 16, BF16, [333], 100, 0, 0, "equal"),
+]
+
+
+@pytest.mark.parametrize("G,D,page,dtype,lens,budget,sinks,recent,kind", EVICT)
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_against_its_definition(G, D, page, dtype, lens, budget, sinks, recent, kind, in_place):
+    _say("evict", G, D, page, dtype, lens, budget, sinks, recent, kind, in_place)
+    g = _gen(budget + D)
+    B = len(lens)
+    made = Made(g, lens, G, D, page, dtype)
+    w = _randn(g, B, G, made.slots).square()
+    if kind == "ties":
+        w = (w * 2).round() / 2
+    elif kind == "equal":
+        w = torch.ones_like(w)
+    elif kind == "special":
+        pick = torch.randint(0, 8, w.shape, generator=g).to(DEV)
+        for i, x in enumerate([math.nan, math.inf, -math.inf, 0.0, -0.0, -1e-42]):
+            w[pick == i] = x
+    positions = torch.stack([torch.stack([torch.randperm(made.slots + 50, generator=g)[: made.slots] for _ in range(G)]) for _ in range(B)]).int().to(DEV)
+    seen = [made.slots + 50 - 3 * b for b in range(B)]
+    w_in, p_in = w.clone(), positions.clone()
+    w_out, p_out = (w, positions) if in_place else (torch.full_like(w, 9.0), torch.full_like(positions, 9))
+    before_k, before_v = made.k.clone(), made.v.clone()
+    got_w, got_p, lengths = fgmp.cache_evict(made.cache, w, positions, _i32(seen), budget, sinks, recent, None if in_place else w_out, None if in_place else p_out)
+    assert got_w is w_out and got_p is p_out
+    assert lengths.tolist() == [min(n, budget) for n in lens]
+    bits = torch.int16 if dtype == BF16 else torch.int32
+    for b, n in enumerate(lens):
+        for h in range(G):
+            now = _evicted(w_in[b, h].tolist(), p_in[b, h].tolist(), n, seen[b], budget, sinks, recent)
+            keep = len(now)
+            assert torch.equal(w_out[b, h, :keep].view(torch.int32), w_in[b, h, now].view(torch.int32)), (b, h)
+            assert torch.equal(p_out[b, h, :keep], p_in[b, h, now]), (b, h)
+            rest_w, rest_p = (w_in[b, h, keep:], p_in[b, h, keep:]) if in_place else (torch.full_like(w_in[b, h, keep:], 9.0), torch.full_like(p_in[b, h, keep:], 9))
+            assert torch.equal(w_out[b, h, keep:].view(torch.int32), rest_w.view(torch.int32)) and torch.equal(p_out[b, h, keep:], rest_p), (b, h)
+            k, v = made.rows(made.k, b, n)[:, h].contiguous(), made.rows(made.v, b, n)[:, h].contiguous()
+            old_k, old_v = made.keys[b][:, h].contiguous(), made.values[b][:, h].contiguous()
+            assert torch.equal(k[:keep].view(bits), old_k[now].view(bits)) and torch.equal(v[:keep].view(bits), old_v[now].view(bits)), (b, h)
+            assert torch.equal(k[keep:].view(bits), old_k[keep:].view(bits)) and torch.equal(v[keep:].view(bits), old_v[keep:].view(bits)), (b, h)
+    # nothing outside of the sequences' slots
+    for x, old in ((made.k, before_k), (made.v, before_v)):
+        unused = torch.ones(x.shape[:2], dtype=torch.bool)
+        for b, n in enumerate(lens):
+            for j in range(0, n, made.size):
+                unused[b if not page else int(made.table[b, j // made.size]), : min(made.size, n - j)] = False
+        u = unused.to(DEV)
+        assert torch.equal(x[u].view(bits), old[u].view(bits))
+
+
+# ---- norms ----
+
+def _norm64(z, w, b, kind, eps):
+    m = z.mean(-1, keepdim=True) if kind == "layer" else torch.zeros_like(z[..., :1])
+    rs = 1.0 / ((z - m).square().mean(-1, keepdim=True) + eps).sqrt()
+    h = (z - m) * rs * w
+    # what a mean off by a rounding of the elements' size does, and a scale off by a few roundings
+    bound = 64 * U32 * (h.abs() + (w * rs).abs() * z.abs().mean(-1, keepdim=True))
+    if b is not None:
+        h, bound = h + b, bound + 2 * U32 * b.abs()
+    return h, bound, rs
+
+
+NORMS = [
+    # rows, width, stream, block, out, kind, gate, act, biases, pre, post
+    (1, 16, BF16, F32, BF16, "rms", None, "none", False, True, True),
+    (3, 4096, BF16, F32, BF16, "rms", "channel", "sigmoid", False, True, True),
+    (5, 2048, F32, BF16, F32, "layer", "full", "silu", True, True, True),
+    (7, 2064, F32, F32, BF16, "layer", "group", "none", True, True, True),
+    (130, 1008, BF16, BF16, F32, "rms", "group", "sigmoid", False, True, True),
+    (2, 8192, F32, F32, F32, "rms", "full", "none", False, True, False),
+    (4, 11008, BF16, F32, BF16, "layer", None, "none", True, False, True),
+    (2, 16384, BF16, BF16, BF16, "rms", "channel", "silu", True, True, True),
+    (3, 32768, F32, BF16, BF16, "layer", "full", "sigmoid", False, True, True),
+    (300, 64, F32, F32, F32, "rms", None, "none", False, True, True),
+    (6, 512, BF16, F32, F32, "rms", None, "none", False, False, False),
+    (9, 4112, F32, F32, F32, "layer", None, "none", True, True, None),   # no block: the first norm
+    (2, 5008, BF16, BF16, BF16, "rms", None, "none", False, True, None),
+]
+
+
+@pytest.mark.parametrize("M,K,xd,od,hd,kind,gate,act,bias,pre,post", NORMS)
+@pytest.mark.parametrize("wide", [False, True])
+def test_norms_against_their_formula(M, K, xd, od, hd, kind, gate, act, bias, pre, post, wide):
+    _say("norm", M, K, xd, od, hd, kind, gate, act, bias, pre, post, wide)
+    g = _gen(M + K)
+
+    def rows(n, dtype, scale=1.0, shift=0.0):
+        return (_randn(g, n, K + (16 if wide else 0)) * scale + shift).to(dtype)[:, :K]
+
+    x = rows(M, xd, 3.0, 1.0)
+    o = rows(M, od, 1.0, 0.25) if post is not None else None
+    gate_rows = {None: 0, "channel": M, "full": 1, "group": 4}[gate]
+    f = rows(-(-M // gate_rows), od) if gate else None
+    vec = [1.0 + 0.1 * _randn(g, K) for _ in range(2)] + [0.1 * _randn(g, K) for _ in range(2)]
+    post_w, post_b = (vec[0] if post else None), (vec[2] if post and bias else None)
+    pre_w, pre_b = (vec[1] if pre else None), (vec[3] if pre and bias else None)
+    a, c, eps = (0.75, -1.5, 1e-4) if o is not None else (1.0, 1.0, 1e-4)
+    y, h = fgmp.block_norm(x, o, post_weight=post_w, post_bias=post_b, pre_weight=pre_w, pre_bias=pre_b, gate=f, gate_act=act, gate_rows=gate_rows,
+                           kind=kind, eps=eps, residual_scale=a, branch_scale=c, h_dtype=hd)
+    d = lambda t: None if t is None else t.double()  # noqa: E731
+    want, bound = x.double(), torch.zeros_like(x, dtype=torch.float64)
+    if o is None:
+        assert y is x
+    else:
+        un, ub = o.double(), torch.zeros_like(o, dtype=torch.float64)
+        if post:
+            un, ub, _ = _norm64(un, d(post_w), d(post_b), kind, eps)
+        if f is not None:
+            e = f.double()[torch.arange(M, device=DEV) // gate_rows]
+            e = {"none": e, "sigmoid": torch.sigmoid(e), "silu": e * torch.sigmoid(e)}[act]
+            un, ub = un * e, ub * e.abs() + 24 * U32 * (un * e).abs()
+        want = a * want + c * un
+        bound = abs(c) * ub + 4 * U32 * ((a * x.double()).abs() + (c * un).abs())
+        assert y.dtype == xd and bool(((y.double() - want).abs() <= bound + _unit(xd) * want.abs()).all())
+    if not pre:
+        assert h is None
+        return
+    hn, hb, rs = _norm64(want, d(pre_w), d(pre_b), kind, eps)
+    # errors of y reach h through the row's scale: directly, and through its sums
+    through = (d(pre_w) * rs).abs() * (bound + bound.mean(-1, keepdim=True)) + hn.abs() * rs * bound.square().mean(-1, keepdim=True).sqrt()
+    assert h.dtype == hd and bool(((h.double() - hn).abs() <= hb + through + _unit(hd) * hn.abs()).all())
+    if o is not None:    # in place, the same bits
+        same, h2 = fgmp.block_norm(x, o, post_weight=post_w, post_bias=post_b, pre_weight=pre_w, pre_bias=pre_b, gate=f, gate_act=act,
+                                   gate_rows=gate_rows, kind=kind, eps=eps, residual_scale=a, branch_scale=c, out=x, h_dtype=hd)
+        assert same is x and torch.equal(x, y) and torch.equal(h2, h)
+
+
+def test_norms_of_zeros_and_of_rows_with_large_means():
+    x = torch.zeros(2, 256, device=DEV)
+    w = torch.ones(256, device=DEV)
+    _, h = fgmp.block_norm(x, pre_weight=w, eps=1e-6)
+    assert bool((h == 0).all())
+    g = _gen(12)
+    # the squares are of what is left after the mean: no digits lost to it beyond those of x itself
+    x = _randn(g, 4, 512) + 4096.0
+    _, h = fgmp.block_norm(x, pre_weight=torch.ones(512, device=DEV), kind="layer")
+    want = torch.nn.functional.layer_norm(x.double(), (512,))
+    assert bool(((h.double() - want).abs() <= 64 * U32 * (want.abs() + 4096.0 * 1.2)).all())
+
+
+def test_a_gate_may_be_one_vector():
+    g = _gen(13)
+    x, o, f = _randn(g, 9, 128), _randn(g, 9, 128), _randn(g, 128)
+    y, h = fgmp.block_norm(x, o, gate=f, gate_act="sigmoid")
+    assert h is None
+    y2, _ = fgmp.block_norm(x, o, gate=f.expand(9, 128).contiguous(), gate_act="sigmoid")
+    assert torch.equal(y, y2)
+
+
+# ---- streams, graphs ----
+
+def _step(g, stream=None):
+    """A step of everything: attention, append, weights, eviction, norm."""
+    B, T, H, G, D = 2, 3, 8, 2, 64
+    made = Made(g, [700, 333], G, D, 16, BF16, room=8)
+    st = {"made": made, "q": _randn(g, B, T, H, D, dtype=BF16), "k": _randn(g, B, T, G, D, dtype=BF16), "v": _randn(g, B, T, G, D, dtype=BF16),
+          "w": _randn(g, B, G, made.slots).square(), "p": torch.arange(made.slots, dtype=torch.int32, device=DEV).repeat(B, G, 1),
+          "positions": _i32([[700, 701, 702], [333, 334, 335]]), "seen": _i32([703, 336]), "x": _randn(g, B * T, H * D), "nw": torch.ones(H * D, device=DEV)}
+    st["out"], st["lse"] = torch.empty_like(st["q"]), torch.empty(B, T, H, device=DEV)
+    st["ws"] = torch.empty(fgmp.tree_attention_workspace_bytes(B, T, H, G, D, made.slots), dtype=torch.uint8, device=DEV)
+    st["ws2"] = torch.empty(fgmp.cache_evict_workspace_bytes(B, G, made.slots, 300), dtype=torch.uint8, device=DEV)
+    st["after"], st["left"] = _i32([0, 0]), _i32([0, 0])
+    st["w1"], st["w2"], st["p2"] = torch.zeros_like(st["w"]), torch.zeros_like(st["w"]), torch.zeros_like(st["p"])
+    st["y"], st["h"] = torch.empty_like(st["x"]), torch.empty(B * T, H * D, dtype=BF16, device=DEV)
+    st["cache"] = fgmp.Cache(made.k, made.v, made.cache.lengths, made.cache.page_table)
+    st["longer"] = fgmp.Cache(made.k, made.v, st["after"], made.cache.page_table)
+    return st
+
+
+def _run_step(st):
+    fgmp.tree_attention(st["q"], st["k"], st["v"], st["cache"], out=st["out"], lse=st["lse"], workspace=st["ws"])
+    fgmp.cache_append(st["k"], st["v"], st["cache"], positions=st["positions"], slot_positions=st["p"], slot_weights=st["w"], lengths_out=st["after"])
+    fgmp.attention_weights(st["q"], st["lse"], st["longer"], st["w"], out=st["w1"])
+    fgmp.cache_evict(st["longer"], st["w1"], st["p"], st["seen"], 300, 4, 20, st["w2"], st["p2"], lengths_out=st["left"], workspace=st["ws2"])
+    fgmp.block_norm(st["x"], st["out"].view(st["x"].shape), pre_weight=st["nw"], out=st["y"], h=st["h"])
+    return [st[n] for n in ("out", "lse", "after", "w1", "w2", "p2", "left", "y", "h")] + [st["made"].k, st["made"].v]
+
+
+def _bits(ts):
+    return [t.clone().view(torch.int16 if t.dtype == BF16 else torch.int32) for t in ts]
+
+
+def test_another_stream_and_a_graph_give_the_same():
+    want = _bits(_run_step(_step(_gen(20))))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    st = _step(_gen(20))
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = _bits(_run_step(st))
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    st = _step(_gen(20))
+    first_k, first_v, first_w = st["made"].k.clone(), st["made"].v.clone(), st["w"].clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = _run_step(st)
+    for replay in range(4):
+        _say("replay", replay)
+        # what a step changes is put back, other inputs take their turn, and other work runs between the replays
+        st["made"].k.copy_(first_k), st["made"].v.copy_(first_v), st["w"].copy_(first_w)
+        for t in outs[:-2]:
+            t.zero_()
+        other = _step(_gen(21 + replay % 2))
+        mine = dict(q=st["q"].clone(), k=st["k"].clone(), v=st["v"].clone())
+        if replay % 2:
+            for n in mine:
+                st[n].copy_(other[n])
+        graph.replay()
+        torch.cuda.synchronize()
+        got = _bits(outs)
+        st["made"].k.copy_(first_k), st["made"].v.copy_(first_v), st["w"].copy_(first_w)
+        eager = _bits(_run_step(st))
+        assert all(torch.equal(a, b) for a, b in zip(got, eager)), replay
+        if replay % 2 == 0:
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), replay
+        for n in mine:
+            st[n].copy_(mine[n])
