@@ -335,7 +335,7 @@ typedef struct {
  *   workspace  >= fgmp_tree_attention_workspace_bytes of the same sizes, with the same max_length or a larger one (the number of slots
  *              where it is 0 here).  No control region is used: it need not be cleared.  May be null where that is 16 bytes.
  * tokens <= 1024.  Sums and softmax statistics are FP32; with BF16 the weights e^(s_j - m) are rounded to BF16 for their product
- * with v, and the sum that divides `out` is that of the rounded ones.
+ * with v (their sum is that of the unrounded ones).
  */
 size_t fgmp_tree_attention_workspace_bytes(int64_t batch, int64_t tokens, int64_t q_heads, int64_t heads, int64_t head_dim,
                                            int64_t max_length);

@@ -24,7 +24,7 @@ CALL_SOURCE = os.path.join(CSRC, "fgmp_call.c")
 CALL = os.path.join(HERE, "_fgmp_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["fgmp_quantize.hip", "fgmp_gemm.hip", "fgmp_gemm_skinny.hip", "fgmp_gemm_stream.hip", "fgmp_gemm_mid.hip",
            "fgmp_gemm_mixed.hip",
-           "fgmp_select.hip", "fgmp_attention.hip", "fgmp_cache.hip", "fgmp_norm.hip", "fgmp_api.hip"]
+           "fgmp_select.hip", "fgmp_attention.hip", "fgmp_attention_wide.hip", "fgmp_cache.hip", "fgmp_norm.hip", "fgmp_api.hip"]
 # -ffp-contract=off: the quantizer's FP32 steps are separately rounded.
 # packed-fp32-ops is switched off for the device compiler on purpose.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

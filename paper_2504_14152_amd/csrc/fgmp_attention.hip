@@ -9,38 +9,14 @@
 // Lane l = 16 g + i then holds, of the weights, row i and keys 4 g .. 4 g + 3 of each 16, and of V the same keys and the
 // elements d = n i .. n i + n - 1 (n = head_dim / 16): 16 lanes load a whole row of V, and BF16 values change places within the
 // lane's registers (32 v_perm for 8 keys x 8 elements).  K is loaded in operand order: 16 rows x 64 bytes an instruction.
-#include <algorithm>
-
-#include "fgmp_cache.hpp"
+#include "fgmp_attention.hpp"
 
 namespace fgmp {
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kWaves = 4;
 constexpr int kMaxTokens = 1024;
-
-struct AttendArgs {
-    CacheView c;
-    const char *q, *k, *v;
-    char *out;
-    float *lse;
-    int64_t q_batch, q_token, q_head, k_batch, k_token, k_head, v_batch, v_token, v_head, o_batch, o_token, o_head;   // bytes
-    const uint64_t *tree;
-    const int32_t *counts;
-    int32_t tokens, q_heads, group, words;
-    int32_t row_blocks, splits;      // workgroups per sequence and head: row blocks x ranges of keys
-    float c2;                        // scale * log2(e)
-    float *part_o, *part_ml;         // partial results of each range: [row][split][dim], [row][split][2]
-};
 
 template <bool kF32>
 struct Elem;
@@ -145,7 +121,7 @@ struct Values {
 // Online softmax state and results of 16 rows: lane 16 g + i has row i; o[m][j] is element n (4 g + j) + m.
 template <int kDim>
 struct RowState {
-    float m, l, lr;   // maximum (of unscaled scores), sum of the weights (lane's keys only) and of the rounded ones
+    float m, l;   // maximum (of unscaled scores), sum of the weights (of the lane's keys)
     f32x4 o[kDim / 16];
 };
 
@@ -160,9 +136,17 @@ __device__ __forceinline__ float over_groups_sum(float x)
     return x + __shfl_xor(x, 32);
 }
 
-// One tile: s[sub][j] are the lane's scores (masked ones -inf), v the values.
+// The softmax of one tile: s[sub][j] are the lane's scores (masked ones -inf); p: the weights as the operand of the second product,
+// relative to the new maximum, by which the state is scaled.
 template <bool kF32, int kDim>
-__device__ __forceinline__ void absorb(RowState<kDim> &st, const f32x4 *s, const Values<kF32, kDim> &v, const bf16x8 *columns, float c2)
+struct Weights;
+template <int kDim>
+struct Weights<false, kDim> { bf16x8 p; };
+template <int kDim>
+struct Weights<true, kDim> { float p[4]; };
+
+template <bool kF32, int kDim>
+__device__ __forceinline__ void weigh(RowState<kDim> &st, const f32x4 *s, Weights<kF32, kDim> &w, float c2)
 {
     constexpr int kSubs = kF32 ? 1 : 2, kPer = kDim / 16;
     float most = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
@@ -173,7 +157,6 @@ __device__ __forceinline__ void absorb(RowState<kDim> &st, const f32x4 *s, const
         const float alpha = st.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((st.m - most) * c2);
         st.m = most;
         st.l *= alpha;
-        st.lr *= alpha;
 #pragma unroll
         for (int m = 0; m < kPer; ++m) st.o[m] *= alpha;
     }
@@ -186,22 +169,29 @@ __device__ __forceinline__ void absorb(RowState<kDim> &st, const f32x4 *s, const
     }
     if constexpr (kF32) {
 #pragma unroll
-        for (int m = 0; m < kPer; ++m)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                st.o[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, v.x[j][m]), p[j], st.o[m], 0, 0, 0);
+        for (int i = 0; i < 4; ++i) w.p[i] = p[i];
     } else {
-        bf16x8 pb;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) pb[i] = (__bf16)p[i];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) st.lr += (float)pb[i];
-#pragma unroll
-        for (int m = 0; m < kPer; ++m) st.o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(columns[m], pb, st.o[m], 0, 0, 0);
+        for (int i = 0; i < 8; ++i) w.p[i] = (__bf16)p[i];
     }
 }
 
-// What absorb() left out of a tile of new tokens: elements of V that are not finite, which rows that do not see their token must
+template <bool kF32, int kDim>
+__device__ __forceinline__ void add_values(RowState<kDim> &st, const Weights<kF32, kDim> &w, const Values<kF32, kDim> &v, const bf16x8 *columns)
+{
+#pragma unroll
+    for (int m = 0; m < kDim / 16; ++m) {
+        if constexpr (kF32) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                st.o[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, v.x[j][m]), w.p[j], st.o[m], 0, 0, 0);
+        } else {
+            st.o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(columns[m], w.p, st.o[m], 0, 0, 0);
+        }
+    }
+}
+
+// What add_values() left out of a tile of new tokens: elements of V that are not finite, which rows that do not see their token must
 // not meet, not even with a weight of zero.  `v` points at the tile's first token.
 template <bool kF32, int kDim>
 __device__ __forceinline__ void add_non_finite(RowState<kDim> &st, const f32x4 *s, uint32_t sees, const char *v, int64_t v_token, int keys, float c2)
@@ -227,41 +217,80 @@ __device__ __forceinline__ void add_non_finite(RowState<kDim> &st, const f32x4 *
     }
 }
 
-// kRows: groups of 16 rows that a workgroup's waves hold, every wave all of them.
+// kRows: groups of 16 rows that a workgroup's waves hold, every wave all of them.  A tile of keys and values is asked for while the one
+// before is worked on: the keys as soon as its scores are there, the values as soon as they have changed places.
 template <bool kF32, int kDim, int kRows>
 __global__ void __launch_bounds__(64 * kWaves) attend_kernel(AttendArgs a)
 {
     constexpr int kSize = Elem<kF32>::kSize, kKeys = Elem<kF32>::kKeys, kSubs = kKeys / 16, kPer = kDim / 16;
     constexpr int kLaneKeys = Values<kF32, kDim>::kLaneKeys;
     __shared__ float merge_o[kWaves][kRows * kPer * 4 * 64];
-    __shared__ float merge_ml[kWaves][kRows][3][16];
+    __shared__ float merge_ml[kWaves][kRows][2][16];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, i = lane & 15;
-    // ranges of keys of one row block next to each other, then row blocks, heads, sequences
-    uint32_t id = blockIdx.x;
-    const int split = id % a.splits;
-    id /= a.splits;
-    const int block = id % a.row_blocks;
-    id /= a.row_blocks;
-    const int h = id % a.c.heads, b = id / a.c.heads;
+    const AttendPlace place(a);
+    if (!place.there) return;
+    const int split = place.split, block = place.block, h = place.h, b = place.b;
 
-    const int32_t n = a.c.length(b);
-    int32_t count = a.counts != nullptr ? a.counts[b] : a.tokens;
-    count = count < 0 ? 0 : count > a.tokens ? a.tokens : count;
+    const int32_t n = a.c.length(b), count = a.count(b);
     const int rows = a.tokens * a.group, first = block * (16 * kRows);
     const bool empty = first >= count * a.group;         // no row of this block belongs to a token that counts
     if (empty && a.splits > 1) return;                   // (written by the launch that joins the ranges)
     const int drafted = a.k != nullptr ? count : 0;
 
-    // this workgroup's tiles: the sequence's are dealt out in equal ranges, the new tokens' go with the last one
-    const int cache_tiles = (n + kKeys - 1) / kKeys;
-    const int per = std::max(kWaves, (cache_tiles + a.splits - 1) / a.splits);
-    const int used = std::max(1, (cache_tiles + per - 1) / per);
+    // this workgroup's tiles; the new tokens' go with the last range
+    const int per = a.range(n), used = a.ranges(n);
     if (split >= used) return;
-    const int end = std::min(cache_tiles, (split + 1) * per);
+    const int end = std::min(a.tiles(n), (split + 1) * per);
     const int draft_tiles = split == used - 1 ? (drafted + kKeys - 1) / kKeys : 0;
 
+    Operand<kF32, kDim> kt[kSubs];
+    Values<kF32, kDim> vt;
+    const uint32_t dv = i * kPer * kSize;
+    const uint32_t step = (uint32_t)a.c.token_stride;    // (16 rows: less than 2^32 bytes)
+    const char *k_at[kSubs], *v_at[kSubs];               // of the tile to be loaded next
+    auto locate = [&](int tile) {
+#pragma unroll
+        for (int sub = 0; sub < kSubs; ++sub) {
+            // (the group of slots behind the last one in use may have no page: read as the one in use)
+            const int64_t at = a.c.group_offset(b, (uint32_t)std::min(kSubs * tile + sub, (n - 1) / 16), h);
+            k_at[sub] = a.c.k + at;
+            v_at[sub] = a.c.v + at;
+        }
+    };
+    // rows behind the last slot in use are read as the last one
+    auto load_keys = [&](int tile) {
+#pragma unroll
+        for (int sub = 0; sub < kSubs; ++sub) {
+            if ((tile + 1) * kKeys <= n) {
+                kt[sub].load(k_at[sub] + ((uint32_t)i * step + 16u * g));
+            } else {
+                const int last = std::min(15, n - 1 - 16 * std::min(kSubs * tile + sub, (n - 1) / 16));
+                kt[sub].load(k_at[sub] + ((uint32_t)std::min(i, last) * step + 16u * g));
+            }
+        }
+    };
+    auto load_values = [&](int tile) {
+#pragma unroll
+        for (int sub = 0; sub < kSubs; ++sub) {
+            if ((tile + 1) * kKeys <= n) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) vt.load(4 * sub + j, v_at[sub] + ((uint32_t)(4 * g + j) * step + dv));
+            } else {
+                const int last = std::min(15, n - 1 - 16 * std::min(kSubs * tile + sub, (n - 1) / 16));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) vt.load(4 * sub + j, v_at[sub] + ((uint32_t)std::min(4 * g + j, last) * step + dv));
+            }
+        }
+    };
+
+    const int begin = empty ? end : split * per + wave;
+    if (begin < end) {
+        locate(begin);
+        load_keys(begin);
+        load_values(begin);
+    }
     int token[kRows];
     Operand<kF32, kDim> q[kRows];
     RowState<kDim> st[kRows];
@@ -272,110 +301,106 @@ __global__ void __launch_bounds__(64 * kWaves) attend_kernel(AttendArgs a)
         const int at = row < rows ? t : 0, head = h * a.group + (row < rows ? row - t * a.group : 0);
         q[r].load(a.q + b * a.q_batch + at * a.q_token + head * a.q_head + 16 * g);
         st[r].m = -INFINITY;
-        st[r].l = st[r].lr = 0.0f;
+        st[r].l = 0.0f;
 #pragma unroll
         for (int m = 0; m < kPer; ++m) st[r].o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    Operand<kF32, kDim> kt[kSubs];
-    Values<kF32, kDim> vt;
-    const int dv = i * kPer * kSize;
-    if (!empty) {
-        for (int tile = split * per + wave; tile < end; tile += kWaves) {
+    for (int tile = begin; tile < end; tile += kWaves) {
+        const int next = tile + kWaves, left = n - tile * kKeys;
+        if (next < end) locate(next);
+        f32x4 s[kRows][kSubs];
 #pragma unroll
-            for (int sub = 0; sub < kSubs; ++sub) {
-                // slots behind the last one in use: their group may have no page; rows are read as the last one in use
-                const int u = std::min(kSubs * tile + sub, (n - 1) / 16), last = std::min(15, n - 1 - 16 * u);
-                const int64_t at = a.c.group_offset(b, (uint32_t)u, h);
-                kt[sub].load(a.c.k + at + (int64_t)std::min(i, last) * a.c.token_stride + 16 * g);
+        for (int r = 0; r < kRows; ++r)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    vt.load(4 * sub + j, a.c.v + at + (int64_t)std::min(4 * g + j, last) * a.c.token_stride + dv);
-            }
-            const int left = n - tile * kKeys;
-            if (left < kKeys) {
-                // what lies behind the sequence must not meet a weight of zero: it might not be finite
+            for (int sub = 0; sub < kSubs; ++sub) s[r][sub] = scores<kF32, kDim>(kt[sub], q[r]);
+        if (next < end) load_keys(next);
+        if (left < kKeys) {
+            // what lies behind the sequence must not meet a weight of zero: it might not be finite
 #pragma unroll
-                for (int j = 0; j < kLaneKeys; ++j)
-                    if (16 * (j / 4) + 4 * g + j % 4 >= left) vt.clear(j);
-            }
-            bf16x8 columns[kPer];
-            if constexpr (!kF32) {
+            for (int j = 0; j < kLaneKeys; ++j) {
+                if (16 * (j / 4) + 4 * g + j % 4 < left) continue;
+                vt.clear(j);
 #pragma unroll
-                for (int m = 0; m < kPer; ++m) columns[m] = vt.column(m);
-            }
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                f32x4 s[kSubs];
-#pragma unroll
-                for (int sub = 0; sub < kSubs; ++sub) {
-                    s[sub] = scores<kF32, kDim>(kt[sub], q[r]);
-                    if (left < kKeys) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (16 * sub + 4 * g + j >= left) s[sub][j] = -INFINITY;
-                    }
-                }
-                absorb<kF32, kDim>(st[r], s, vt, columns, a.c2);
+                for (int r = 0; r < kRows; ++r) s[r][j / 4][j % 4] = -INFINITY;
             }
         }
-        for (int tile = wave; tile < draft_tiles; tile += kWaves) {
-            const int start = tile * kKeys, last = drafted - 1 - start;
+        Weights<kF32, kDim> w[kRows];
+        if constexpr (kF32) {
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) weigh<kF32, kDim>(st[r], s[r], w[r], a.c2);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) add_values<kF32, kDim>(st[r], w[r], vt, nullptr);
+            if (next < end) load_values(next);
+        } else {
+            bf16x8 columns[kPer];
+#pragma unroll
+            for (int m = 0; m < kPer; ++m) columns[m] = vt.column(m);
+            if (next < end) load_values(next);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) weigh<kF32, kDim>(st[r], s[r], w[r], a.c2);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) add_values<kF32, kDim>(st[r], w[r], vt, columns);
+        }
+    }
+    // (the first of them to the wave behind the one that had the last tile of the range)
+    for (int tile = empty ? draft_tiles : (wave + kWaves - (end - split * per) % kWaves) % kWaves; tile < draft_tiles; tile += kWaves) {
+        const int start = tile * kKeys, last = drafted - 1 - start;
+#pragma unroll
+        for (int sub = 0; sub < kSubs; ++sub) {
+            kt[sub].load(a.k + b * a.k_batch + (start + std::min(16 * sub + i, last)) * a.k_token + h * a.k_head + 16 * g);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                vt.load(4 * sub + j, a.v + b * a.v_batch + (start + std::min(16 * sub + 4 * g + j, last)) * a.v_token + h * a.v_head + dv);
+        }
+#pragma unroll
+        for (int j = 0; j < kLaneKeys; ++j)
+            if (16 * (j / 4) + 4 * g + j % 4 > last) vt.clear(j);
+        const bool finite = __all(vt.all_finite());
+        if (!finite) vt.clear_non_finite();
+        bf16x8 columns[kPer];
+        if constexpr (!kF32) {
+#pragma unroll
+            for (int m = 0; m < kPer; ++m) columns[m] = vt.column(m);
+        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            // bit j: the lane's row sees new token start + j
+            uint32_t sees = 0u;
+            if (token[r] >= 0) {
+                if (a.tree != nullptr) {
+                    const uint64_t word = a.tree[((int64_t)b * a.tokens + token[r]) * a.words + (start >> 6)];
+                    sees = (uint32_t)(word >> (start & 63));
+                } else {
+                    const int upto = token[r] - start;
+                    sees = upto >= 31 ? 0xFFFFFFFFu : upto < 0 ? 0u : (2u << upto) - 1u;
+                }
+                if (last < 31) sees &= (2u << last) - 1u;
+            }
+            f32x4 s[kSubs];
 #pragma unroll
             for (int sub = 0; sub < kSubs; ++sub) {
-                kt[sub].load(a.k + b * a.k_batch + (start + std::min(16 * sub + i, last)) * a.k_token + h * a.k_head + 16 * g);
+                s[sub] = scores<kF32, kDim>(kt[sub], q[r]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    vt.load(4 * sub + j, a.v + b * a.v_batch + (start + std::min(16 * sub + 4 * g + j, last)) * a.v_token + h * a.v_head + dv);
+                    if ((sees >> (16 * sub + 4 * g + j) & 1u) == 0u) s[sub][j] = -INFINITY;
             }
-#pragma unroll
-            for (int j = 0; j < kLaneKeys; ++j)
-                if (16 * (j / 4) + 4 * g + j % 4 > last) vt.clear(j);
-            const bool finite = __all(vt.all_finite());
-            if (!finite) vt.clear_non_finite();
-            bf16x8 columns[kPer];
-            if constexpr (!kF32) {
-#pragma unroll
-                for (int m = 0; m < kPer; ++m) columns[m] = vt.column(m);
-            }
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                // bit j: the lane's row sees new token start + j
-                uint32_t sees = 0u;
-                if (token[r] >= 0) {
-                    if (a.tree != nullptr) {
-                        const uint64_t word = a.tree[((int64_t)b * a.tokens + token[r]) * a.words + (start >> 6)];
-                        sees = (uint32_t)(word >> (start & 63));
-                    } else {
-                        const int upto = token[r] - start;
-                        sees = upto >= 31 ? 0xFFFFFFFFu : upto < 0 ? 0u : (2u << upto) - 1u;
-                    }
-                    if (last < 31) sees &= (2u << last) - 1u;
-                }
-                f32x4 s[kSubs];
-#pragma unroll
-                for (int sub = 0; sub < kSubs; ++sub) {
-                    s[sub] = scores<kF32, kDim>(kt[sub], q[r]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if ((sees >> (16 * sub + 4 * g + j) & 1u) == 0u) s[sub][j] = -INFINITY;
-                }
-                absorb<kF32, kDim>(st[r], s, vt, columns, a.c2);
-                if (!finite)
-                    add_non_finite<kF32, kDim>(st[r], s, sees, a.v + b * a.v_batch + start * a.v_token + h * a.v_head, a.v_token,
-                                               std::min(kKeys, last + 1), a.c2);
-            }
+            Weights<kF32, kDim> w;
+            weigh<kF32, kDim>(st[r], s, w, a.c2);
+            add_values<kF32, kDim>(st[r], w, vt, columns);
+            if (!finite)
+                add_non_finite<kF32, kDim>(st[r], s, sees, a.v + b * a.v_batch + start * a.v_token + h * a.v_head, a.v_token,
+                                           std::min(kKeys, last + 1), a.c2);
         }
     }
 
     // join the waves: every one holds all rows over keys of its own
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
-        const float l = over_groups_sum(st[r].l), lr = kF32 ? l : over_groups_sum(st[r].lr);
+        const float l = over_groups_sum(st[r].l);
         if (g == 0) {
             merge_ml[wave][r][0][i] = st[r].m;
             merge_ml[wave][r][1][i] = l;
-            merge_ml[wave][r][2][i] = lr;
         }
 #pragma unroll
         for (int m = 0; m < kPer; ++m)
@@ -389,17 +414,16 @@ __global__ void __launch_bounds__(64 * kWaves) attend_kernel(AttendArgs a)
         float most = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) most = fmaxf(most, merge_ml[w][r][0][i]);
-        float f[kWaves], l = 0.0f, lr = 0.0f;
+        float f[kWaves], l = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const float m = merge_ml[w][r][0][i];
             f[w] = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - most) * a.c2);
             l += merge_ml[w][r][1][i] * f[w];
-            lr += merge_ml[w][r][2][i] * f[w];
         }
         const int t = row / a.group, head = h * a.group + row - t * a.group;
-        const int64_t place = ((int64_t)b * a.tokens + t) * a.q_heads + head;   // (of rows that exist)
-        const float inverse = lr > 0.0f ? 1.0f / lr : lr == 0.0f ? 0.0f : lr;    // (NaN stays)
+        const int64_t at = ((int64_t)b * a.tokens + t) * a.q_heads + head;   // (of rows that exist)
+        const float inverse = inverse_sum(l);
 #pragma unroll
         for (int m4 = 0; m4 < kPer / kWaves; ++m4) {
             const int m = wave * (kPer / kWaves) + m4;
@@ -409,7 +433,7 @@ __global__ void __launch_bounds__(64 * kWaves) attend_kernel(AttendArgs a)
             if (row < rows) {
                 if (a.splits > 1) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) a.part_o[(place * a.splits + split) * kDim + kPer * (4 * g + j) + m] = o[j];
+                    for (int j = 0; j < 4; ++j) a.part_o[(at * a.splits + split) * kDim + kPer * (4 * g + j) + m] = o[j];
                 } else {
                     char *to = a.out + b * a.o_batch + t * a.o_token + head * a.o_head;
 #pragma unroll
@@ -424,51 +448,81 @@ __global__ void __launch_bounds__(64 * kWaves) attend_kernel(AttendArgs a)
         }
         if (wave == 0 && g == 0 && row < rows) {
             if (a.splits > 1) {
-                float *ml = a.part_ml + (place * a.splits + split) * 4;
+                float *ml = a.part_ml + (at * a.splits + split) * 2;
                 ml[0] = most;
                 ml[1] = l;
-                ml[2] = lr;
             } else {
-                a.lse[place] = t >= count || l == 0.0f ? -INFINITY : (most * a.c2 + __builtin_amdgcn_logf(l)) * kLn2;
+                a.lse[at] = t < count ? logsumexp(most, l, a.c2) : -INFINITY;
             }
         }
     }
 }
 
-// Joins the ranges of keys: one wave per row.
-template <bool kF32, int kDim>
-__global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int64_t all_rows)
+template <int kN>
+struct FloatsOf {
+    typedef float type __attribute__((ext_vector_type(kN)));
+};
+
+// Joins the ranges of keys.  kWavesPerRow waves to a row: a lane holds the maximum and sum of one range (of every 64), and each wave adds
+// up every kWavesPerRow-th range.  One wave does for up to 16 ranges (12800 rows of 4 ranges, head_dim 128: 9.5 us, 20.5 with four waves, of
+// which three have hardly anything to do), four for more (64 rows of 64 ranges: 7 us, 36 with one).
+template <bool kF32, int kDim, int kWavesPerRow>
+__global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int64_t rows)
 {
-    constexpr int kKeys = Elem<kF32>::kKeys, kPer = kDim / 64;
-    const int lane = threadIdx.x & 63;
-    const int64_t place = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (place >= all_rows) return;
-    const int head = (int)(place % a.q_heads);
-    const int64_t bt = place / a.q_heads;
-    const int t = (int)(bt % a.tokens), b = (int)(bt / a.tokens);
-    int32_t count = a.counts != nullptr ? a.counts[b] : a.tokens;
-    const int cache_tiles = (a.c.length(b) + kKeys - 1) / kKeys;
-    const int per = std::max(kWaves, (cache_tiles + a.splits - 1) / a.splits);
-    const int used = t < count ? std::max(1, (cache_tiles + per - 1) / per) : 0;
-    const float *ml = a.part_ml + place * a.splits * 4, *po = a.part_o + place * a.splits * kDim + lane * kPer;
+    constexpr int kPer = kDim / 64, kRowsHere = 4 / kWavesPerRow;
+    using part = typename FloatsOf<kPer>::type;
+    __shared__ part sums[kWavesPerRow][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = wave % kWavesPerRow;
+    const int64_t at = (int64_t)blockIdx.x * kRowsHere + wave / kWavesPerRow;
+    if (kWavesPerRow == 1 && at >= rows) return;
+    const int head = (int)((uint32_t)at % (uint32_t)a.q_heads);
+    const uint32_t bt = (uint32_t)at / (uint32_t)a.q_heads;
+    const int t = (int)(bt % (uint32_t)a.tokens), b = (int)(bt / (uint32_t)a.tokens);
+    const int used = t < a.count(b) ? a.ranges(a.c.length(b)) : 0;
+    const float *ml = a.part_ml + at * a.splits * 2;
+    const part *po = reinterpret_cast<const part *>(a.part_o + at * a.splits * kDim) + lane;
     float most = -INFINITY;
-    for (int s = 0; s < used; ++s) most = fmaxf(most, ml[4 * s]);
-    float l = 0.0f, lr = 0.0f, o[kPer] = {};
-    for (int s = 0; s < used; ++s) {
-        const float m = ml[4 * s], f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - most) * a.c2);
-        l += ml[4 * s + 1] * f;
-        lr += ml[4 * s + 2] * f;
+    for (int s = lane; s < used; s += 64) most = fmaxf(most, ml[2 * s]);
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) o[e] += po[s * kDim + e] * f;
+    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+    float l = 0.0f;
+    part o = {};
+    for (int start = 0; start < used; start += 64) {
+        float f = 0.0f;
+        if (start + lane < used) {
+            const float m = ml[2 * (start + lane)];
+            f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - most) * a.c2);
+            l += ml[2 * (start + lane) + 1] * f;
+        }
+        const int here = std::min(64, used - start);
+        for (int first = share; first < here; first += 4 * kWavesPerRow) {
+            part x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = po[(start + std::min(first + kWavesPerRow * j, here - 1)) * 64];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float factor = __shfl(f, first + kWavesPerRow * j);
+                if (first + kWavesPerRow * j < here) o += x[j] * factor;
+            }
+        }
     }
-    const float inverse = lr > 0.0f ? 1.0f / lr : lr == 0.0f ? 0.0f : lr;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+    if constexpr (kWavesPerRow > 1) {
+        sums[wave][lane] = o;
+        __syncthreads();
+        if (wave != 0) return;
+        o = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    }
+    o *= inverse_sum(l);
     char *to = a.out + b * a.o_batch + t * a.o_token + head * a.o_head;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
-        if constexpr (kF32) reinterpret_cast<float *>(to)[lane * kPer + e] = o[e] * inverse;
-        else reinterpret_cast<__bf16 *>(to)[lane * kPer + e] = (__bf16)(o[e] * inverse);
+        const float x = o[e];
+        if constexpr (kF32) reinterpret_cast<float *>(to)[lane * kPer + e] = x;
+        else reinterpret_cast<__bf16 *>(to)[lane * kPer + e] = (__bf16)x;
     }
-    if (lane == 0) a.lse[place] = l == 0.0f ? -INFINITY : (most * a.c2 + __builtin_amdgcn_logf(l)) * kLn2;
+    if (lane == 0) a.lse[at] = logsumexp(most, l, a.c2);
 }
 
 // ---- attention weights of accepted tokens ----
@@ -573,39 +627,60 @@ __global__ void __launch_bounds__(64 * kWaves) weights_kernel(WeightArgs a)
     }
 }
 
-// How a call is shared out: groups of 16 rows per workgroup, row blocks, ranges of keys.
+// How a call is shared out.  Up to 32 rows, and in the types and sizes that the kernel for many rows does not have, a workgroup's waves
+// all have the same rows; that kernel's have 32 each.
 struct AttendPlan {
-    int row_groups;
+    int waves_of_rows;      // of the kernel for many rows; 0: the other one
+    int row_groups;         // groups of 16 rows, of the other one
+    int tile_keys, min_tiles;
     int64_t row_blocks, splits;
+    int64_t units, workgroups;   // ranges of all heads and sequences; in eights, and for each row block
 };
 
-AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t heads, int64_t head_dim, int64_t max_length)
+AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t heads, int64_t head_dim, bool f32, int64_t max_length)
 {
-    AttendPlan p;
+    AttendPlan p = {};
     const int64_t groups = (tokens * (q_heads / heads) + 15) / 16;
-    p.row_groups = 1;
-    (void)head_dim;
-    p.row_blocks = (groups + p.row_groups - 1) / p.row_groups;
-    const int64_t whole = batch * heads * p.row_blocks;
-    // at least 128 keys in a range, and about four workgroups for each compute unit
-    p.splits = std::max<int64_t>(1, std::min((max_length + 127) / 128, (1024 + whole - 1) / whole));
+    int64_t want;   // workgroups that the chip holds at a time
+    if (!f32 && head_dim != 256 && groups > 2) {
+        p.waves_of_rows = groups <= 8 ? 4 : 8;
+        p.row_blocks = (groups + 15) / 16;
+        p.tile_keys = kWideKeys;
+        p.min_tiles = 4;
+        want = p.waves_of_rows == 8 ? 256 : 512;
+    } else {
+        // as many rows as the registers of a wave hold, in blocks of equal size
+        const int64_t most = head_dim == 256 ? 1 : 2;
+        p.row_blocks = (groups + most - 1) / most;
+        p.row_groups = (int)((groups + p.row_blocks - 1) / p.row_blocks);
+        p.tile_keys = f32 ? Elem<true>::kKeys : Elem<false>::kKeys;
+        p.min_tiles = 128 / p.tile_keys;
+        want = p.row_groups == 1 ? 1024 : 512;
+    }
+    const int64_t whole = batch * heads * p.row_blocks, least = (int64_t)p.tile_keys * p.min_tiles;
+    p.splits = std::max<int64_t>(1, std::min((max_length + least - 1) / least, (want + whole - 1) / whole));
+    p.units = batch * heads * p.splits;
+    p.workgroups = (p.units + 7) / 8 * 8 * p.row_blocks;
     return p;
 }
 
 size_t attend_bytes(const AttendPlan &p, int64_t rows, int64_t head_dim)
 {
-    return p.splits > 1 ? (size_t)(rows * p.splits * (head_dim + 4) * 4) : 0;
+    return p.splits > 1 ? (size_t)(rows * p.splits * (head_dim + 2) * 4) : 0;
 }
 
 template <bool kF32, int kDim>
 void attend_launch(const AttendArgs &a, const AttendPlan &p, hipStream_t st)
 {
-    const dim3 grid((unsigned)(a.c.batch * a.c.heads * p.row_blocks * p.splits));
-    attend_kernel<kF32, kDim, 1><<<grid, 64 * kWaves, 0, st>>>(a);
-    if (p.splits > 1) {
-        const int64_t rows = (int64_t)a.c.batch * a.tokens * a.q_heads;
-        join_kernel<kF32, kDim><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(a, rows);
+    const dim3 grid((unsigned)p.workgroups);
+    if (p.waves_of_rows > 0) attend_wide(a, p.waves_of_rows, (uint32_t)p.workgroups, st);
+    else if (p.row_groups == 1) attend_kernel<kF32, kDim, 1><<<grid, 64 * kWaves, 0, st>>>(a);
+    if constexpr (kDim != 256) {
+        if (p.row_groups == 2) attend_kernel<kF32, kDim, 2><<<grid, 64 * kWaves, 0, st>>>(a);
     }
+    const int64_t rows = (int64_t)a.c.batch * a.tokens * a.q_heads;
+    if (p.splits > 16) join_kernel<kF32, kDim, 4><<<dim3((unsigned)rows), 256, 0, st>>>(a, rows);
+    else if (p.splits > 1) join_kernel<kF32, kDim, 1><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(a, rows);
 }
 
 }  // namespace
@@ -621,7 +696,11 @@ size_t fgmp_tree_attention_workspace_bytes(int64_t batch, int64_t tokens, int64_
     if (batch <= 0 || tokens <= 0 || tokens > kMaxTokens || heads <= 0 || q_heads <= 0 || q_heads % heads != 0 || batch > 65535 ||
         q_heads > 65535 || max_length < 0 || max_length > (int64_t)1 << 30 || (head_dim != 64 && head_dim != 128 && head_dim != 256))
         return 0;
-    return std::max<size_t>(16, attend_bytes(attend_plan(batch, tokens, q_heads, heads, head_dim, max_length), batch * tokens * q_heads, head_dim));
+    // (the cache's type is not known here: whichever needs more)
+    const AttendPlan p = attend_plan(batch, tokens, q_heads, heads, head_dim, false, max_length);
+    const AttendPlan f = attend_plan(batch, tokens, q_heads, heads, head_dim, true, max_length);
+    const int64_t rows = batch * tokens * q_heads;
+    return std::max<size_t>(16, std::max(attend_bytes(p, rows, head_dim), attend_bytes(f, rows, head_dim)));
 }
 
 fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, const fgmp_heads_t *v, int64_t tokens, int64_t q_heads,
@@ -643,7 +722,7 @@ fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, 
         if ((rc = check_heads(v, a.c.batch, tokens, a.c.heads, dim, size, false)) != FGMP_OK) return rc;
     }
     if (max_length == 0 || max_length > a.c.slots) max_length = a.c.slots;
-    const AttendPlan p = attend_plan(a.c.batch, tokens, q_heads, a.c.heads, dim, max_length);
+    const AttendPlan p = attend_plan(a.c.batch, tokens, q_heads, a.c.heads, dim, cache->dtype == FGMP_F32, max_length);
     const int64_t rows = a.c.batch * tokens * q_heads;
     const size_t need = attend_bytes(p, rows, dim);
     if (need > 0) {
@@ -651,7 +730,7 @@ fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, 
         if (!aligned16(workspace)) return FGMP_ERR_BAD_ALIGN;
         if (workspace_bytes < need) return FGMP_ERR_BUFFER_TOO_SMALL;
     }
-    if (a.c.batch * a.c.heads * p.row_blocks * p.splits >= (int64_t)1 << 31) return FGMP_ERR_UNSUPPORTED;
+    if (p.workgroups >= (int64_t)1 << 31 || rows >= (int64_t)1 << 31) return FGMP_ERR_UNSUPPORTED;
     a.q = static_cast<const char *>(q->data);
     a.q_batch = q->batch_stride * size, a.q_token = q->token_stride * size, a.q_head = q->head_stride * size;
     a.out = static_cast<char *>(out->data);
@@ -669,8 +748,11 @@ fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, 
     a.q_heads = (int32_t)q_heads;
     a.group = (int32_t)(q_heads / a.c.heads);
     a.words = (int32_t)((tokens + 63) / 64);
-    a.row_blocks = (int32_t)p.row_blocks;
+    a.row_blocks = (uint32_t)p.row_blocks;
+    a.units = (uint32_t)p.units;
     a.splits = (int32_t)p.splits;
+    a.tile_keys = p.tile_keys;
+    a.min_tiles = p.min_tiles;
     a.c2 = scale * kLog2e;
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = a.part_o + rows * p.splits * dim;

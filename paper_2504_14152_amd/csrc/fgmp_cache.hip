@@ -36,9 +36,13 @@ fgmp_status_t check_cache(const fgmp_cache_t *c, CacheView *view)
     view->pages = (uint32_t)c->pages;
     view->pages_per_sequence = (uint32_t)c->pages_per_sequence;
     view->page_groups = paged ? (uint32_t)(c->page_size / kSlotGroup) : 0u;
-    view->page_shift = -1;
-    for (int i = 0; i < 31; ++i)
-        if (view->page_groups == 1u << i) view->page_shift = i;
+    if (paged) {
+        // with 2^k >= d the factor 2^(27 + k) / d, rounded up, is off by less than 1 in 2^27 of a quotient's unit for u < 2^27
+        uint32_t k = 0;
+        while ((1u << k) < view->page_groups) ++k;
+        view->group_shift = 27u + k;
+        view->group_factor = (uint32_t)((((uint64_t)1 << view->group_shift) + view->page_groups - 1) / view->page_groups);
+    }
     view->slots = (int32_t)slots;
     view->batch = c->batch;
     view->heads = c->heads;

@@ -9,13 +9,13 @@ constexpr int kSlotGroup = 16;
 
 struct CacheView {
     char *k, *v;
-    const int32_t *page_table;
+    const int32_t *page_table;   // null: sequence b's slots are page b
     const int32_t *lengths;
     int64_t page_stride, token_stride, head_stride;   // bytes
     int64_t table_stride;
     uint32_t pages, pages_per_sequence;
-    uint32_t page_groups;        // slot groups per page; 0: no page table, sequence b's slots are page b
-    int32_t page_shift;          // log2 of page_groups, -1 where it is no power of two
+    uint32_t page_groups;        // slot groups per page
+    uint32_t group_factor, group_shift;   // u / page_groups = u * factor >> shift for u < 2^27; factor 0 without a page table (one page, all slots)
     int32_t slots;               // of a sequence
     int32_t batch, heads, head_dim;
 
@@ -24,21 +24,32 @@ struct CacheView {
         const int32_t n = lengths[b];
         return n < 0 ? 0 : n > slots ? slots : n;
     }
-    // Byte offset of row 0 of slot group `u` of sequence b and head h (b, u, h uniform over the wave).  `*there` is cleared
-    // where the page table's entry is none of the cache's pages (page 0 is given instead).
+    // Which entry of its row of the page table slot group `u` falls under; `*row`: its first slot in that page.
+    __device__ __forceinline__ uint32_t entry_of(uint32_t u, uint32_t *row) const
+    {
+        const uint32_t at = (uint32_t)((uint64_t)u * group_factor >> group_shift);   // u / page_groups
+        *row = (u - at * page_groups) * kSlotGroup;
+        return at;
+    }
+    // The page table is not written while a kernel runs: read as constant memory, through the scalar cache where `at` is uniform.
+    __device__ __forceinline__ uint32_t page_of(int b, uint32_t at) const
+    {
+        typedef const __attribute__((address_space(4))) int32_t *constant;
+        return page_table != nullptr ? (uint32_t)((constant)(uintptr_t)page_table)[b * table_stride + at] : (uint32_t)b;
+    }
+    // Byte offset of row `row` of page `page` of a head; `*there`: whether there is such a page (if not, page 0 is given instead).
+    __device__ __forceinline__ int64_t offset(uint32_t page, uint32_t row, int h, bool *there = nullptr) const
+    {
+        if (there != nullptr) *there = page < pages;
+        page = page < pages ? page : 0u;
+        return (int64_t)page * page_stride + (int64_t)row * token_stride + (int64_t)h * head_stride;
+    }
+    // ... of row 0 of slot group `u` of sequence b.
     __device__ __forceinline__ int64_t group_offset(int b, uint32_t u, int h, bool *there = nullptr) const
     {
-        uint32_t page = (uint32_t)b, row = u;
-        if (page_groups != 0u) {
-            const uint32_t at = page_shift >= 0 ? u >> page_shift : u / page_groups;
-            row = u - at * page_groups;
-            page = (uint32_t)page_table[b * table_stride + at];
-            if (page >= pages) {
-                page = 0u;
-                if (there != nullptr) *there = false;
-            }
-        }
-        return (int64_t)page * page_stride + (int64_t)(row * kSlotGroup) * token_stride + (int64_t)h * head_stride;
+        uint32_t row;
+        const uint32_t at = entry_of(u, &row);
+        return offset(page_of(b, at), row, h, there);
     }
 };
 

@@ -151,6 +151,12 @@ ATTEND = [
     (BF16, 128, 16, 2, 33, [1030, 64], 256, True, [33, 20]),
     (BF16, 128, 2, 2, 65, [90], 16, True, None),
     (BF16, 128, 3, 1, 130, [257], 64, False, [129]),
+    (BF16, 64, 8, 1, 12, [63, 64, 65], 16, True, [12, 9, 4]),
+    (BF16, 64, 16, 1, 15, [700, 3], 0, False, None),
+    (BF16, 64, 8, 1, 70, [130, 129], 48, True, [70, 64]),
+    (BF16, 128, 4, 1, 9, [0, 127, 128], 80, True, [9, 0, 5]),
+    (BF16, 128, 12, 2, 10, [1000], 64, False, None),
+    (BF16, 128, 24, 2, 12, [2049, 511], 32, True, [12, 7]),
     (F32, 64, 4, 4, 1, [1, 700], 0, False, None),
     (F32, 128, 8, 2, 4, [0, 15, 16, 17], 16, True, [4, 4, 0, 3]),
     (F32, 256, 2, 1, 7, [123], 48, True, None),
@@ -181,11 +187,12 @@ def test_attention_against_its_formula(dtype, D, H, G, T, lens, page, tree, coun
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-def test_hidden_tokens_reach_no_row_whatever_they_hold(dtype, bad):
+@pytest.mark.parametrize("H,G,D", [(4, 2, 64), (1, 1, 64), (3, 1, 128), (10, 2, 128), (12, 1, 64)])
+def test_hidden_tokens_reach_no_row_whatever_they_hold(H, G, D, dtype, bad):
     """A new token whose key and value are not finite, seen by some rows and not by others: the others' results are as if it
     were not there; those that see it get no finite result."""
     g = _gen(3)
-    B, T, H, G, D = 1, 21, 4, 2, 64
+    B, T = 1, 21
     made = Made(g, [77], G, D, 16, dtype)
     q, k, v = _randn(g, B, T, H, D, dtype=dtype), _randn(g, B, T, G, D, dtype=dtype), _randn(g, B, T, G, D, dtype=dtype)
     words, sees = _random_tree(g, B, T)
@@ -238,7 +245,7 @@ def test_attention_of_tensors_that_are_parts_of_others(dtype):
     _compare_attention(out, lse, q, made, shared, shared, _chain(B, T), [T] * B, D ** -0.5, H // G)
 
 
-@pytest.mark.parametrize("dtype,H,T", [(BF16, 8, 1), (BF16, 16, 9), (F32, 8, 2), (BF16, 2, 64)])
+@pytest.mark.parametrize("dtype,H,T", [(BF16, 8, 1), (BF16, 16, 9), (F32, 8, 2), (BF16, 2, 64), (BF16, 16, 2), (BF16, 6, 8), (BF16, 20, 17)])
 def test_ranges_of_a_long_cache_join(dtype, H, T):
     """Lengths around every way to share a sequence out, and hints that are too small."""
     g = _gen(6)
