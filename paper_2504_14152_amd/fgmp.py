@@ -155,6 +155,8 @@ def _load(path: str) -> ctypes.CDLL:
     L.fgmp_quant_gemm_fused.argtypes = [vp, ctypes.c_int, i64, i64, i64, vp, f32, f32, vp, i64, vp, i64,
                                         vp, sz, vp]
     L.fused_entry = ctypes.cast(L.fgmp_quant_gemm_fused, ctypes.c_void_p).value
+    L.entries = {n: ctypes.cast(getattr(L, "fgmp_" + n), ctypes.c_void_p).value
+                 for n in ("tree_attention", "attention_weights", "cache_append", "cache_evict", "block_norm")}
     L.fgmp_quant_gemm_fused_static_scratch.restype = ctypes.c_int
     L.fgmp_quant_gemm_fused_static_scratch.argtypes = [vp, ctypes.c_int, i64, i64, i64, vp, f32, f32, vp, i64, vp, i64, vp]
     L.fgmp_unpack_canonical.restype = ctypes.c_int
@@ -558,6 +560,23 @@ def selftest_decode_table(fmt: int, device="cuda"):
 
 # ---- between the products of a layer: attention over a cache, the cache's upkeep, norms ----
 
+# the element types that the extension module tells apart, in its order
+_TYPES = (torch.float32, torch.bfloat16, torch.int32, torch.int64, torch.uint8)
+
+
+def _handed(name: str, *args) -> bool:
+    """Whether the extension module took a call's arguments as they are (and the call went well); otherwise nothing has happened, and the
+    general path has something to make, to refuse or to say."""
+    if _call is None:
+        return False
+    rc = getattr(_call, name)(lib().entries[name], _TYPES, *args, _stream())
+    if rc is None:
+        return False
+    if rc != 0:
+        _check(rc, "fgmp_" + name)
+    return True
+
+
 class Cache:
     """Keys and values of a batch of sequences (fgmp_cache_t): `k` and `v` pages x page_size x heads x head_dim, of the same type
     and strides, head_dim contiguous; `page_table` batch x pages per sequence (int32), or None: sequence b's slots are page b;
@@ -581,6 +600,7 @@ class Cache:
                                     k.stride(0), k.stride(1), k.stride(2), _ptr(page_table), 0 if page_table is None else page_table.stride(0),
                                     None)
         self._ref = ctypes.byref(self._struct)
+        self._handle = (ctypes.addressof(self._struct), self.batch, heads, dim, self.slots, k.dtype)
         self.lengths = lengths
 
     @property
@@ -640,6 +660,9 @@ def tree_attention(q: torch.Tensor, k: torch.Tensor | None, v: torch.Tensor | No
     """(out, lse) of new tokens' attention over a cache and each other: q batch x tokens x query heads x head_dim; k, v batch x tokens x
     heads x head_dim, or None.  `tree`: batch x tokens x words (int64, see tree_words), None for a chain; `counts` (int32): new tokens
     of each sequence; `scale` 1 / sqrt(head_dim) unless given; `max_length`: the longest sequence, where the caller knows it."""
+    if out is not None and lse is not None and workspace is not None and scale is not None and _handed(
+            "tree_attention", q, k, v, cache._handle, tree, counts, scale, max_length, out, lse, workspace):
+        return out, lse
     _require_cuda(q, k, v, tree, counts, out, lse, workspace)
     if q.dim() != 4 or (k is None) != (v is None):
         raise FgmpError("q: batch x tokens x heads x head_dim; k and v: both or neither")
@@ -671,6 +694,9 @@ def attention_weights(q: torch.Tensor, lse: torch.Tensor, cache: Cache, weights:
     """`weights` (batch x heads x slots, float32) and what the accepted tokens' attention adds to it, in `out` (`weights` itself unless
     given): call it after cache_append, with the q and lse that tree_attention took and gave.  `rows` (int32, batch x accepted): which
     rows of q were accepted; `counts` (int32): how many of them."""
+    if scale is not None and _handed("attention_weights", q, lse, cache._handle, weights, rows, counts, scale, max_length,
+                                     weights if out is None else out):
+        return weights if out is None else out
     _require_cuda(q, lse, weights, rows, counts, out)
     if q.dim() != 4 or q.shape[0] != cache.batch or q.shape[3] != cache.head_dim:
         raise FgmpError("q does not match the cache")
@@ -701,6 +727,8 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, cache: Cache, rows: torch.Ten
     """Keys and values of accepted tokens (`rows`, `counts` as attention_weights; k, v as tree_attention, float32 too) into the next slots
     of the cache; returns the new lengths, for cache.lengths.  `positions` (int32, batch x tokens) go to `slot_positions` (int32, batch x
     heads x slots); `slot_weights` (float32) of new slots become 0."""
+    if lengths_out is not None and _handed("cache_append", k, v, cache._handle, rows, counts, positions, slot_positions, slot_weights, lengths_out):
+        return lengths_out
     _require_cuda(k, v, rows, counts, positions, slot_positions, slot_weights, lengths_out)
     if k.dim() != 4 or k.dtype != v.dtype:
         raise FgmpError("k and v: batch x tokens x heads x head_dim, of one type")
@@ -730,9 +758,12 @@ def cache_evict(cache: Cache, weights: torch.Tensor, positions: torch.Tensor, se
                 lengths_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """Cuts every sequence to `budget` slots by accumulated attention weight (fgmp_cache_evict): keys and values move within the cache;
     returns (weights, positions, lengths), the first two in place unless `weights_out` and `positions_out` are given."""
-    _require_cuda(weights, positions, seen, weights_out, positions_out, lengths_out, workspace)
     weights_out = weights if weights_out is None else weights_out
     positions_out = positions if positions_out is None else positions_out
+    if lengths_out is not None and workspace is not None and _handed(
+            "cache_evict", cache._handle, weights, positions, seen, budget, sinks, recent, weights_out, positions_out, lengths_out, workspace):
+        return weights_out, positions_out, lengths_out
+    _require_cuda(weights, positions, seen, weights_out, positions_out, lengths_out, workspace)
     shape = (cache.batch, cache.heads, weights.shape[-1])
     _check_f32(weights, "weights", shape)
     _check_f32(weights_out, "weights_out", shape)
@@ -764,6 +795,10 @@ def block_norm(x: torch.Tensor, o: torch.Tensor | None = None, post_weight: torc
     """(y, h) of the norms around a block (fgmp_block_norm): y = residual_scale x + branch_scale act(gate) N(o; post), x itself where `o` is
     None; h = N(y; pre), None without `pre_weight`.  x, o M x K; `gate` K values (one per channel) or rows of K, each for `gate_rows` rows of
     x (1 unless given).  `out` (may be x) and `h` are made where they are not given, h in `h_dtype` or x's type."""
+    if (out is None) == (o is None) and (h is None) == (pre_weight is None) and h_dtype is None and kind in NORMS and gate_act in GATES and _handed(
+            "block_norm", x, o, gate, gate_rows or 1, GATES[gate_act], post_weight, post_bias, pre_weight, pre_bias, NORMS[kind], eps, residual_scale,
+            branch_scale, out, h):
+        return (x if o is None else out), h
     _require_cuda(x, o, post_weight, post_bias, pre_weight, pre_bias, gate, out, h)
     M, K = x.shape
     for t in (post_weight, post_bias, pre_weight, pre_bias):

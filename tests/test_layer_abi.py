@@ -142,3 +142,125 @@ def test_the_binding_wants_gpu_tensors():
         fgmp.Cache(x, x, n)
     with pytest.raises(fgmp.FgmpError):
         fgmp.block_norm(torch.zeros(1, 16), pre_weight=torch.ones(16))
+
+
+# ---- the extension module's way ----
+
+class _Tensor:
+    """What the binding asks of a GPU tensor, without one."""
+
+    def __init__(self, at, shape, dtype=torch.float32, stride=None, cuda=True):
+        self.at, self.shape, self.dtype, self.is_cuda = at, torch.Size(shape), dtype, cuda
+        self._stride = stride or torch.empty(shape, device="meta").stride()
+
+    def data_ptr(self):
+        return self.at
+
+    def stride(self):
+        return self._stride
+
+
+class _Handle:
+    def __init__(self):
+        self.struct = fgmp._CacheStruct()
+        self.fast = (ctypes.addressof(self.struct), 2, 3, 64, 40, torch.bfloat16)
+
+
+I64, VP, F, SZ, I = ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_size_t, ctypes.c_int
+HEADS = ctypes.POINTER(fgmp._HeadsStruct)
+_NUMBERS = {ctypes.c_int64, ctypes.c_float, ctypes.c_size_t, ctypes.c_int}
+
+
+def _told(name, given, *argtypes):
+    """What the entry point is called with when the extension is given `given`, and the answer; heads as tuples."""
+    got = []
+
+    def entry(*a):
+        got.append(tuple((x.contents.data, x.contents.batch_stride, x.contents.token_stride, x.contents.head_stride) if t is HEADS and x else
+                         None if t is HEADS else x for x, t in zip(a, argtypes)))
+        return -4
+
+    f = ctypes.CFUNCTYPE(ctypes.c_int, *argtypes)(entry)
+    fgmp.lib()
+    rc = getattr(fgmp._call, name)(ctypes.cast(f, VP).value, fgmp._TYPES, *given, 0x77)
+    assert (rc is None) == (not got) and rc in (None, -4)
+    return got[0] if got else None
+
+
+def _t(at, *shape, dtype=torch.float32, **more):
+    return _Tensor(at, shape, dtype, **more)
+
+
+BF, I32 = torch.bfloat16, torch.int32
+
+
+def test_the_extension_hands_on_attention():
+    h = _Handle()
+    q, out = _t(16, 2, 5, 6, 64, dtype=BF, stride=(4000, 800, 64, 1)), _t(32, 2, 5, 6, 64, dtype=BF)
+    k, v = _t(48, 2, 5, 3, 64, dtype=BF), _t(64, 2, 5, 3, 64, dtype=BF, stride=(9000, 1000, 128, 1))
+    tree, counts, lse, ws = _t(80, 2, 5, 1, dtype=torch.int64), _t(96, 2, dtype=I32), _t(112, 2, 5, 6), _t(128, 999, dtype=torch.uint8)
+    types = (HEADS, HEADS, HEADS, I64, I64, VP, VP, VP, F, I64, HEADS, VP, VP, SZ, VP)
+    given = [q, k, v, h.fast, tree, counts, 0.25, 33, out, lse, ws]
+    want = ((16, 4000, 800, 64), (48, 960, 192, 64), (64, 9000, 1000, 128), 5, 6, h.fast[0], 80, 96, 0.25, 33, (32, 1920, 384, 64), 112, 128, 999, 0x77)
+    assert _told("tree_attention", given, *types) == want
+    assert _told("tree_attention", given[:1] + [None, None] + given[3:4] + [None, None] + given[6:], *types) == want[:1] + (None, None) + want[3:6] + (None, None) + want[8:]
+    bad = {0: [_t(16, 2, 5, 6, 64), _t(16, 2, 5, 6, 32, dtype=BF), _t(16, 3, 5, 6, 64, dtype=BF), _t(16, 2, 5, 6, 64, dtype=BF, cuda=False),
+               _t(16, 2, 5, 6, 64, dtype=BF, stride=(1920, 384, 1, 6)), None, 7],
+           1: [_t(48, 2, 4, 3, 64, dtype=BF), _t(48, 2, 5, 6, 64, dtype=BF), None], 4: [_t(80, 2, 5, 2, dtype=torch.int64), _t(80, 2, 5, 1, dtype=I32)],
+           5: [_t(96, 2, dtype=torch.int64), _t(96, 3, dtype=I32), _t(96, 2, dtype=I32, stride=(2,))], 6: [None, "x"], 7: [1.5, None],
+           8: [_t(32, 2, 5, 6, 64)], 9: [_t(112, 2, 6, 5), _t(112, 2, 5, 6, stride=(60, 12, 2)), None], 10: [None, _t(128, 9, dtype=I32)]}
+    for at, values in bad.items():
+        for value in values:
+            assert _told("tree_attention", given[:at] + [value] + given[at + 1:], *types) is None, (at, value)
+    # 70 tokens take two words
+    g70 = [_t(16, 2, 70, 6, 64, dtype=BF), None, None, h.fast, _t(80, 2, 70, 2, dtype=torch.int64), None, 1, 0, _t(32, 2, 70, 6, 64, dtype=BF), _t(112, 2, 70, 6), ws]
+    assert _told("tree_attention", g70, *types)[3:9] == (70, 6, h.fast[0], 80, None, 1.0)
+
+
+def test_the_extension_hands_on_weights_append_and_evict():
+    h = _Handle()
+    types = (HEADS, VP, I64, I64, VP, VP, I64, VP, F, I64, VP, VP, I64, VP)
+    given = [_t(16, 2, 5, 6, 64, dtype=BF), _t(32, 2, 5, 6), h.fast, _t(48, 2, 3, 50), _t(64, 2, 4, dtype=I32), _t(80, 2, dtype=I32), 0.5, 0, _t(96, 2, 3, 50)]
+    want = ((16, 1920, 384, 64), 32, 5, 6, h.fast[0], 64, 4, 80, 0.5, 0, 48, 96, 50, 0x77)
+    assert _told("attention_weights", given, *types) == want
+    assert _told("attention_weights", given[:4] + [None, None] + given[6:], *types)[5:8] == (None, 5, None)
+    for at, value in [(3, _t(48, 2, 4, 50)), (8, _t(96, 2, 3, 51)), (4, _t(64, 3, 4, dtype=I32)), (1, _t(32, 2, 5, 6, dtype=BF))]:
+        assert _told("attention_weights", given[:at] + [value] + given[at + 1:], *types) is None, at
+
+    types = (HEADS, HEADS, I, I64, VP, VP, I64, VP, VP, VP, VP, I64, VP, VP)
+    given = [_t(16, 2, 5, 3, 64), _t(32, 2, 5, 3, 64), h.fast, None, _t(48, 2, dtype=I32), _t(64, 2, 5, dtype=I32), _t(80, 2, 3, 41, dtype=I32), _t(96, 2, 3, 41), _t(112, 2, dtype=I32)]
+    want = ((16, 960, 192, 64), (32, 960, 192, 64), 0, 5, h.fast[0], None, 5, 48, 64, 80, 96, 41, 112, 0x77)
+    assert _told("cache_append", given, *types) == want
+    both = _told("cache_append", [_t(16, 2, 5, 3, 64, dtype=BF), _t(32, 2, 5, 3, 64, dtype=BF)] + given[2:5] + [None, None, None] + given[8:], *types)
+    assert both[2] == 1 and both[8:12] == (None, None, None, 0)
+    for at, value in [(0, _t(16, 2, 5, 3, 64, dtype=BF)), (1, _t(32, 2, 5, 4, 64)), (6, _t(80, 2, 3, 40, dtype=I32)), (8, None)]:
+        assert _told("cache_append", given[:at] + [value] + given[at + 1:], *types) is None, at
+
+    types = (VP, VP, VP, I64, VP, I64, I64, I64, VP, VP, VP, VP, SZ, VP)
+    given = [h.fast, _t(16, 2, 3, 40), _t(32, 2, 3, 40, dtype=I32), _t(48, 2, dtype=I32), 30, 4, 5, _t(64, 2, 3, 40), _t(80, 2, 3, 40, dtype=I32),
+             _t(96, 2, dtype=I32), _t(112, 77, dtype=torch.uint8)]
+    assert _told("cache_evict", given, *types) == (h.fast[0], 16, 32, 40, 48, 30, 4, 5, 64, 80, 96, 112, 77, 0x77)
+    for at, value in [(1, _t(16, 2, 3, 39)), (2, _t(32, 2, 3, 40)), (4, 1.0), (7, None), (9, _t(96, 3, dtype=I32)), (10, None)]:
+        assert _told("cache_evict", given[:at] + [value] + given[at + 1:], *types) is None, at
+
+
+def test_the_extension_hands_on_norms():
+    types = (VP, I, I64, VP, I, I64, VP, I64, I64, I, I64, I64, VP, VP, VP, VP, I, F, F, F, VP, I64, VP, I, I64, VP)
+    vec = [_t(200 + 16 * i, 32) for i in range(4)]
+    given = [_t(16, 5, 32, dtype=BF, stride=(40, 1)), _t(32, 5, 32), _t(48, 3, 32, stride=(48, 1)), 2, 1, *vec, 1, 0.5, 0.25, 2, _t(64, 5, 32, dtype=BF), _t(80, 5, 32)]
+    want = (16, 1, 40, 32, 0, 32, 48, 48, 2, 1, 5, 32, 200, 216, 232, 248, 1, 0.5, 0.25, 2.0, 64, 32, 80, 0, 32, 0x77)
+    assert _told("block_norm", given, *types) == want
+    first = _told("block_norm", [given[0], None, None, 1, 0, None, None, vec[2], None, 0, 1e-5, 1.0, 1.0, None, given[14]], *types)
+    assert first[3] is None and first[6] is None and first[12:16] == (None, None, 232, None) and first[20] is None
+    for at, value in [(0, _t(16, 5, 32, dtype=I32)), (1, _t(32, 4, 32)), (2, _t(48, 2, 32)), (2, _t(48, 3, 32, dtype=BF)), (2, _t(48, 32)), (3, 0), (5, _t(200, 31)),
+                      (5, _t(200, 32, dtype=BF)), (13, _t(64, 5, 32)), (14, _t(80, 5, 32, stride=(1, 5)))]:
+        assert _told("block_norm", given[:at] + [value] + given[at + 1:], *types) is None, (at, value)
+
+
+@pytest.mark.parametrize("name,count", [("tree_attention", 14), ("attention_weights", 12), ("cache_append", 12), ("cache_evict", 14), ("block_norm", 18)])
+def test_the_extension_counts_its_arguments(name, count):
+    fgmp.lib()
+    f = getattr(fgmp._call, name)
+    with pytest.raises(TypeError):
+        f(*[None] * (count - 1))
+    assert f(*[None] * count) is None and f(0, (1, 2), *[None] * (count - 2)) is None
