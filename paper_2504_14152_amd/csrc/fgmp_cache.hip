@@ -166,24 +166,27 @@ struct EvictArgs {
     int64_t room;
 };
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr int kRankBits = 11, kRankBins = 1 << kRankBits;   // 32 bits in digits of 11, 11 and 10
 
-// Sum of `mine` over the threads before this one in the workgroup, and over all of them.
+// Sum of `mine` over the threads before this one in the workgroup, and over all of them.  One barrier: two calls that follow each other
+// need parts of their own.
+template <int kWaves>
 __device__ __forceinline__ uint32_t exclusive_sum(uint32_t mine, uint32_t *part, uint32_t *all)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // within rows of 16 lanes, then the rows' sums on to the rows behind
     uint32_t incl = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t v = __shfl_up(incl, d);
-        incl += lane >= d ? v : 0u;
-    }
-    __syncthreads();
+    incl += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)incl, 0x111, 0xF, 0xF, false);
+    incl += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)incl, 0x112, 0xF, 0xF, false);
+    incl += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)incl, 0x114, 0xF, 0xF, false);
+    incl += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)incl, 0x118, 0xF, 0xF, false);
+    incl += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)incl, 0x142, 0xA, 0xF, false);
+    incl += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)incl, 0x143, 0xC, 0xF, false);
     if (lane == 63) part[wave] = incl;
     __syncthreads();
     uint32_t before = 0u, sum = 0u;
 #pragma unroll
-    for (int w = 0; w < kSelectWaves; ++w) {
+    for (int w = 0; w < kWaves; ++w) {
         const uint32_t v = part[w];
         before += w < wave ? v : 0u;
         sum += v;
@@ -192,79 +195,141 @@ __device__ __forceinline__ uint32_t exclusive_sum(uint32_t mine, uint32_t *part,
     return before + incl - mine;
 }
 
-// One workgroup per sequence and head: the rank of the budget-th entry by radix selection (four digits of eight bits), then
-// who stays, and the i-th entry that stays behind the budget is paired with the i-th place that becomes free below it.
-__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(EvictArgs a)
+// One workgroup per sequence and head: the rank of the budget-th entry by radix selection, then who stays, and the i-th entry that stays
+// behind the budget is paired with the i-th place that becomes free below it.  A thread holds the ranks of 4 kQuads slots next to each other
+// in registers (of that many times kThreads slots at a time where a sequence has more: then they are read again in every pass), so weights
+// and positions are read once, and the order over the workgroup takes one sum over threads instead of one for every kThreads slots.
+// Weights share a few exponents: digits of 11 bits take mantissa bits in from the first pass on, and copies of the bins keep the lanes of a
+// wave apart.  64 heads of 16381 slots: 62 us with digits of 8 bits and two sums for every 1024 slots, 19 so (64 of 1031: 11 and 6.5); what
+// is left is latency, of the first loads, of bins and barriers.
+template <int kThreads, int kQuads>
+__global__ void __launch_bounds__(kThreads) evict_select_kernel(EvictArgs a)
 {
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t part[kSelectWaves];
+    constexpr int kWaves = kThreads / 64, kCopies = kThreads / 256, kSpan = 4 * kQuads, kBinsPer = kRankBins / kThreads;
+    __shared__ uint32_t hist[kCopies][kRankBins];
+    __shared__ uint32_t part[2][kWaves];
     __shared__ uint32_t found[2];
     const int b = blockIdx.x / a.c.heads, h = blockIdx.x % a.c.heads, tid = threadIdx.x;
     const int64_t at = (int64_t)blockIdx.x * a.slot_stride;
+    const int64_t newest = (int64_t)a.seen[b] - a.recent;
     const int32_t n = a.c.length(b), keep = n < a.budget ? n : a.budget;
     if (h == 0 && tid == 0) a.lengths_out[b] = keep;
     const float *w = a.weights + at;
     const int32_t *pos = a.positions + at;
-    if (n <= a.budget) {
-        for (int i = tid; i < n; i += kSelectThreads) {
-            const float x = w[i];
-            const int32_t p = pos[i];
-            a.weights_out[at + i] = x;
-            a.positions_out[at + i] = p;
+    float *w_out = a.weights_out + at;
+    int32_t *pos_out = a.positions_out + at;
+    const bool quads = (((uintptr_t)w | (uintptr_t)pos | (uintptr_t)w_out | (uintptr_t)pos_out) & 15u) == 0u;   // (16 bytes at a time)
+    uint32_t rank[kSpan];
+    // `copy`: and what lies below the new length goes to the outputs, places that become free included (they are filled by the moves)
+    auto load = [&](int start, bool copy) {
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q) {
+            const int i = start + tid * kSpan + 4 * q;
+            float x[4] = {};
+            int32_t p[4] = {};
+            if (quads && i + 4 <= n) {
+                const float4 f = *reinterpret_cast<const float4 *>(w + i);
+                const int4 e = *reinterpret_cast<const int4 *>(pos + i);
+                x[0] = f.x, x[1] = f.y, x[2] = f.z, x[3] = f.w;
+                p[0] = e.x, p[1] = e.y, p[2] = e.z, p[3] = e.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (i + j < n) x[j] = w[i + j], p[j] = pos[i + j];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) rank[4 * q + j] = p[j] < a.sinks || p[j] >= newest ? 0xFFFFFFFFu : rank_of(x[j]);
+            if (copy) {
+                if (quads && i + 4 <= keep) {
+                    *reinterpret_cast<float4 *>(w_out + i) = make_float4(x[0], x[1], x[2], x[3]);
+                    *reinterpret_cast<int4 *>(pos_out + i) = make_int4(p[0], p[1], p[2], p[3]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (i + j < keep) w_out[i + j] = x[j], pos_out[i + j] = p[j];
+                }
+            }
         }
+    };
+    const bool once = n <= kSpan * kThreads, copies = w != w_out || pos != pos_out;
+    if (n <= a.budget) {
+        if (copies)
+            for (int start = 0; start < n; start += kSpan * kThreads) load(start, true);
         if (tid == 0) a.moved[blockIdx.x] = 0u;
         return;
     }
-    const int64_t newest = (int64_t)a.seen[b] - a.recent;
-    auto rank = [&](int i) {
-        const int32_t p = pos[i];
-        return p < a.sinks || p >= newest ? 0xFFFFFFFFu : rank_of(w[i]);
-    };
+    if (once) load(0, copies);
     uint32_t prefix = 0u, wanted = (uint32_t)a.budget;   // the wanted-th largest among those that match the prefix
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0u;
-        __syncthreads();
-        for (int i = tid; i < n; i += kSelectThreads) {
-            const uint32_t r = rank(i);
-            if (shift == 24 || (r >> (shift + 8)) == prefix) atomicAdd(&hist[(r >> shift) & 255u], 1u);
+    for (int i = tid; i < kCopies * kRankBins; i += kThreads) (&hist[0][0])[i] = 0u;
+    __syncthreads();
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : kRankBits;
+        for (int start = 0; start < n; start += kSpan * kThreads) {
+            if (!once) load(start, copies && pass == 0);
+#pragma unroll
+            for (int j = 0; j < kSpan; ++j)
+                if (start + tid * kSpan + j < n && (pass == 0 || rank[j] >> (shift + bits) == prefix))
+                    atomicAdd(&hist[tid % kCopies][(rank[j] >> shift) & ((1u << bits) - 1u)], 1u);
         }
         __syncthreads();
-        // thread t holds the bin 255 - t: the bins above it are those of the threads before
-        uint32_t all;
-        const uint32_t mine = tid < 256 ? hist[255 - tid] : 0u;
-        const uint32_t above = exclusive_sum(mine, part, &all);
-        if (tid < 256 && above < wanted && wanted <= above + mine) {
-            found[0] = (prefix << 8) | (uint32_t)(255 - tid);
-            found[1] = wanted - above;
+        // thread t holds kBinsPer bins, from the top: the bins above them are those of the threads before
+        const int top = kRankBins - 1 - kBinsPer * tid;
+        uint32_t bin[kBinsPer], mine = 0u, all;
+#pragma unroll
+        for (int i = 0; i < kBinsPer; ++i) {
+            bin[i] = 0u;
+#pragma unroll
+            for (int c = 0; c < kCopies; ++c) bin[i] += hist[c][top - i];
+            mine += bin[i];
         }
+        uint32_t above = exclusive_sum<kWaves>(mine, part[pass & 1], &all);
+#pragma unroll
+        for (int i = 0; i < kBinsPer; ++i) {
+            if (above < wanted && wanted <= above + bin[i]) {
+                found[0] = (prefix << bits) | (uint32_t)(top - i);
+                found[1] = wanted - above;
+            }
+            above += bin[i];
+        }
+        if (pass < 2)
+            for (int i = tid; i < kCopies * kRankBins; i += kThreads) (&hist[0][0])[i] = 0u;
         __syncthreads();
         prefix = found[0];
         wanted = found[1];
-        __syncthreads();
     }
     // entries above `prefix` stay, and the first `wanted` of those that equal it
     int2 *moves = a.moves + blockIdx.x * a.room;
     uint32_t equal = 0u, holes = 0u, movers = 0u;
-    for (int start = 0; start < n; start += kSelectThreads) {
-        const int i = start + tid;
-        uint32_t r = 0u;
-        if (i < n) r = rank(i);
-        const bool same = i < n && r == prefix;
-        uint32_t sum;
-        const uint32_t before = exclusive_sum(same ? 1u : 0u, part, &sum);
-        const bool stays = i < n && (r > prefix || (same && equal + before < wanted));
+    for (int start = 0; start < n; start += kSpan * kThreads) {
+        if (!once) load(start, false);
+        const int first = start + tid * kSpan;
+        uint32_t same = 0u, sum;
+#pragma unroll
+        for (int j = 0; j < kSpan; ++j) same += first + j < n && rank[j] == prefix ? 1u : 0u;
+        uint32_t left = equal + exclusive_sum<kWaves>(same, part[1], &sum);   // of those equal, how many come before
         equal += sum;
-        const bool hole = i < a.budget && !stays, mover = i >= a.budget && stays;   // (i < n: n > budget, and stays)
-        const uint32_t order = exclusive_sum((hole ? 1u : 0u) + (mover ? 0x10000u : 0u), part, &sum);
-        if (hole) moves[holes + (order & 0xFFFFu)].y = i;
-        if (mover) moves[movers + (order >> 16)].x = i;
+        uint32_t stays = 0u, mine = 0u;   // (holes in the lower half, movers in the upper one: no more than 16384 of either)
+#pragma unroll
+        for (int j = 0; j < kSpan; ++j) {
+            const int i = first + j;
+            bool stay = i < n && rank[j] > prefix;
+            if (i < n && rank[j] == prefix) stay = left++ < wanted;
+            stays |= stay ? 1u << j : 0u;
+            mine += (i < a.budget && !stay ? 1u : 0u) + (i >= a.budget && stay ? 0x10000u : 0u);   // (the budget is below n)
+        }
+        const uint32_t order = exclusive_sum<kWaves>(mine, part[0], &sum);
+        uint32_t hole = holes + (order & 0xFFFFu), mover = movers + (order >> 16);
         holes += sum & 0xFFFFu;
         movers += sum >> 16;
-        if (stays && i < a.budget) {
-            const float x = w[i];
-            const int32_t p = pos[i];
-            a.weights_out[at + i] = x;
-            a.positions_out[at + i] = p;
+#pragma unroll
+        for (int j = 0; j < kSpan; ++j) {
+            const int i = first + j;
+            if ((stays >> j & 1u) != 0u) {
+                if (i >= a.budget) moves[mover++].x = i;
+            } else if (i < a.budget) {
+                moves[hole++].y = i;
+            }
         }
     }
     if (tid == 0) a.moved[blockIdx.x] = holes;
@@ -402,7 +467,9 @@ fgmp_status_t fgmp_cache_evict(const fgmp_cache_t *cache, const float *weights, 
     const int64_t per_head = std::max<int64_t>(1, std::min<int64_t>(steps, std::max<int64_t>(1, 4096 / pairs)));
     if (pairs * per_head >= (int64_t)1 << 31) return FGMP_ERR_UNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    evict_select_kernel<<<dim3((unsigned)pairs), kSelectThreads, 0, st>>>(a);
+    if (a.c.slots <= 2048) evict_select_kernel<512, 1><<<dim3((unsigned)pairs), 512, 0, st>>>(a);
+    else if (a.c.slots <= 8192) evict_select_kernel<1024, 2><<<dim3((unsigned)pairs), 1024, 0, st>>>(a);
+    else evict_select_kernel<1024, 4><<<dim3((unsigned)pairs), 1024, 0, st>>>(a);
     if (a.room > 0) evict_move_kernel<<<dim3((unsigned)(pairs * per_head)), 256, 0, st>>>(a, (int)per_head, piece_shift);
     return launched();
 }
