@@ -528,10 +528,11 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int64_t rows)
 // ---- attention weights of accepted tokens ----
 //
 // The first product alone, S = Q K^T, with rows along the registers: the sum over rows is then within a lane, but for its last
-// step over the four lane groups.  A wave holds 16 kWeightKeys keys in registers and walks over the accepted rows, of which the workgroup
-// stages kStage at a time in LDS, in operand order.  No sum is shared between waves: the order of additions is fixed.
+// step over the four lane groups.  A wave holds 16 kWeightKeys keys in registers, asks for its next ones, and walks over the accepted rows,
+// which the workgroup stages in LDS in operand order: once where they are no more than kStage, for every block of keys else.  No sum is
+// shared between waves: the order of additions is fixed.
 
-constexpr int kWeightKeys = 2, kStage = 32;
+constexpr int kWeightKeys = 2, kStage = 64, kWeightWorkgroups = 2048;
 
 struct WeightArgs {
     CacheView c;
@@ -563,39 +564,56 @@ __global__ void __launch_bounds__(64 * kWaves) weights_kernel(WeightArgs a)
     int32_t count = a.counts != nullptr ? a.counts[b] : a.accepted;
     count = count < 0 ? 0 : count > a.accepted ? a.accepted : count;
     const int rows = count * a.group;
-    for (int first = block * kBlock; first < n; first += a.blocks * kBlock) {
-        const int mine = first + wave * 16 * kWeightKeys;
-        Operand<kF32, kDim> kt[kWeightKeys];
+    // rows start .. start + kStage - 1; of those that there are not, whole groups of 16 are left as they are
+    auto put = [&](int start) {
+        for (int p = tid; p < kStage / 16 * kPieces * 64; p += 64 * kWaves) {
+            if (start + p / (kPieces * 64) * 16 >= rows) break;
+            const int r = start + p / (kPieces * 64) * 16 + (p & 15);
+            u32x4 x = {0u, 0u, 0u, 0u};
+            if (r < rows) {
+                const int t = r / a.group, row = a.rows != nullptr ? a.rows[b * (int64_t)a.accepted + t] : t;
+                if ((uint32_t)row < (uint32_t)a.tokens)
+                    x = *reinterpret_cast<const u32x4 *>(a.q + b * a.q_batch + row * a.q_token + (h * a.group + r - t * a.group) * a.q_head +
+                                                         p / 64 % kPieces * 64 + (p / 16 & 3) * 16);
+            }
+            stage[p / (kPieces * 64)][p / 64 % kPieces][p & 63] = x;
+        }
+        if (tid < kStage) {
+            const int r = start + tid, t = r / a.group;
+            float lse = INFINITY;
+            if (r < rows) {
+                const int row = a.rows != nullptr ? a.rows[b * (int64_t)a.accepted + t] : t;
+                if ((uint32_t)row < (uint32_t)a.tokens) lse = a.lse[((int64_t)b * a.tokens + row) * a.q_heads + h * a.group + r - t * a.group] * kLog2e;
+            }
+            stage_lse[tid] = lse;
+            stage_end[tid] = n - count + t + 1;
+        }
+    };
+    auto load = [&](int first, Operand<kF32, kDim> *k) {
 #pragma unroll
         for (int s = 0; s < kWeightKeys; ++s) {
-            const int u = std::min(mine / 16 + s, (n - 1) / 16), last = std::min(15, n - 1 - 16 * u);
-            kt[s].load(a.c.k + a.c.group_offset(b, (uint32_t)u, h) + (int64_t)std::min(i, last) * a.c.token_stride + 16 * g);
+            const int u = std::min(first / 16 + wave * kWeightKeys + s, (n - 1) / 16), last = std::min(15, n - 1 - 16 * u);
+            k[s].load(a.c.k + a.c.group_offset(b, (uint32_t)u, h) + ((uint32_t)std::min(i, last) * (uint32_t)a.c.token_stride + 16u * g));
         }
+    };
+    const bool once = rows <= kStage;
+    Operand<kF32, kDim> kt[kWeightKeys];
+    if (block * kBlock < n) load(block * kBlock, kt);
+    if (once) {
+        put(0);
+        __syncthreads();
+    }
+    for (int first = block * kBlock; first < n; first += a.blocks * kBlock) {
+        const int mine = first + wave * 16 * kWeightKeys, next = first + a.blocks * kBlock;
+        Operand<kF32, kDim> ahead[kWeightKeys];
+        if (next < n) load(next, ahead);
         float sum[kWeightKeys] = {};
         for (int start = 0; start < rows; start += kStage) {
-            __syncthreads();
-            for (int p = tid; p < kStage / 16 * kPieces * 64; p += 64 * kWaves) {
-                const int r = start + p / (kPieces * 64) * 16 + (p & 15);
-                u32x4 x = {0u, 0u, 0u, 0u};
-                if (r < rows) {
-                    const int t = r / a.group, row = a.rows != nullptr ? a.rows[b * (int64_t)a.accepted + t] : t;
-                    if ((uint32_t)row < (uint32_t)a.tokens)
-                        x = *reinterpret_cast<const u32x4 *>(a.q + b * a.q_batch + row * a.q_token + (h * a.group + r - t * a.group) * a.q_head +
-                                                             p / 64 % kPieces * 64 + (p / 16 & 3) * 16);
-                }
-                stage[p / (kPieces * 64)][p / 64 % kPieces][p & 63] = x;
+            if (!once) {
+                __syncthreads();
+                put(start);
+                __syncthreads();
             }
-            if (tid < kStage) {
-                const int r = start + tid, t = r / a.group;
-                float lse = INFINITY;
-                if (r < rows) {
-                    const int row = a.rows != nullptr ? a.rows[b * (int64_t)a.accepted + t] : t;
-                    if ((uint32_t)row < (uint32_t)a.tokens) lse = a.lse[((int64_t)b * a.tokens + row) * a.q_heads + h * a.group + r - t * a.group] * kLog2e;
-                }
-                stage_lse[tid] = lse;
-                stage_end[tid] = n - count + t + 1;
-            }
-            __syncthreads();
 #pragma unroll 1
             for (int r = 0; r < kStage / 16 && start + 16 * r < rows; ++r) {
                 Operand<kF32, kDim> q;
@@ -624,6 +642,8 @@ __global__ void __launch_bounds__(64 * kWaves) weights_kernel(WeightArgs a)
                 a.out[at] = a.weights[at] + total;
             }
         }
+#pragma unroll
+        for (int s = 0; s < kWeightKeys; ++s) kt[s] = ahead[s];
     }
 }
 
@@ -786,7 +806,8 @@ fgmp_status_t fgmp_attention_weights(const fgmp_heads_t *q, const float *lse, in
     if (max_length == 0 || max_length > a.c.slots) max_length = a.c.slots;
     constexpr int kBlock = 16 * kWeightKeys * kWaves;
     const int64_t pairs = (int64_t)a.c.batch * a.c.heads;
-    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>((max_length + kBlock - 1) / kBlock, ((int64_t)1 << 30) / pairs));
+    // (about as many workgroups as the chip holds at a time)
+    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>((max_length + kBlock - 1) / kBlock, (kWeightWorkgroups + pairs - 1) / pairs));
     a.q = static_cast<const char *>(q->data);
     a.q_batch = q->batch_stride * size, a.q_token = q->token_stride * size, a.q_head = q->head_stride * size;
     a.lse = lse;
