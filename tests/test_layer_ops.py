@@ -554,6 +554,8 @@ NORMS = [
     (2, 16384, BF16, BF16, BF16, "rms", "channel", "silu", True, True, True),
     (3, 32768, F32, BF16, BF16, "layer", "full", "sigmoid", False, True, True),
     (300, 64, F32, F32, F32, "rms", None, "none", False, True, True),
+    (77, 256, BF16, F32, BF16, "layer", "group", "sigmoid", True, True, True),
+    (9, 208, F32, BF16, F32, "rms", "full", "none", False, True, True),
     (6, 512, BF16, F32, F32, "rms", None, "none", False, False, False),
     (9, 4112, F32, F32, F32, "layer", None, "none", True, True, None),   # no block: the first norm
     (2, 5008, BF16, BF16, BF16, "rms", None, "none", False, True, None),
