@@ -220,7 +220,7 @@ __device__ __forceinline__ void add_non_finite(RowState<kDim> &st, const f32x4 *
 // kRows: groups of 16 rows that a workgroup's waves hold, every wave all of them.  A tile of keys and values is asked for while the one
 // before is worked on: the keys as soon as its scores are there, the values as soon as they have changed places.
 template <bool kF32, int kDim, int kRows>
-__global__ void __launch_bounds__(64 * kWaves) attend_kernel(AttendArgs a)
+__global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(AttendArgs a)
 {
     constexpr int kSize = Elem<kF32>::kSize, kKeys = Elem<kF32>::kKeys, kSubs = kKeys / 16, kPer = kDim / 16;
     constexpr int kLaneKeys = Values<kF32, kDim>::kLaneKeys;
@@ -331,6 +331,17 @@ __global__ void __launch_bounds__(64 * kWaves) attend_kernel(AttendArgs a)
             for (int r = 0; r < kRows; ++r) weigh<kF32, kDim>(st[r], s[r], w[r], a.c2);
 #pragma unroll
             for (int r = 0; r < kRows; ++r) add_values<kF32, kDim>(st[r], w[r], vt, nullptr);
+            if (next < end) load_values(next);
+        } else if constexpr (kRows > 1) {
+            // (no registers for the values in both orders)
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) weigh<kF32, kDim>(st[r], s[r], w[r], a.c2);
+#pragma unroll
+            for (int m = 0; m < kPer; ++m) {
+                const bf16x8 column = vt.column(m);
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) st[r].o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(column, w[r].p, st[r].o[m], 0, 0, 0);
+            }
             if (next < end) load_values(next);
         } else {
             bf16x8 columns[kPer];

@@ -19,10 +19,11 @@ struct Tile {
     static constexpr int kPieces = kDim / 8;                       // 16-byte pieces of a key
     u32x4 k[kWideKeys * kPieces];                                  // [key][piece ^ key]
     u32x4 v[kDim * kWideKeys / 8];                                 // [element][piece ^ element]
-    static __device__ __forceinline__ int key_piece(int key, int piece) { return key * kPieces + (piece ^ (key & 7)); }
+    // LDS gives 16 lanes 16 bytes each in a cycle: a piece of 16 keys in a row, or of 16 elements, lies in 16 different places of 256 bytes
+    static __device__ __forceinline__ int key_piece(int key, int piece) { return key * kPieces + (piece ^ (kPieces == 16 ? key & 15 : key >> 1 & 7)); }
     // 16 keys are the k index of a matrix instruction: piece 2 s + g is what lane half g takes of the s-th 16, the groups
     // of four keys 4 s + g and 4 s + g + 2
-    static __device__ __forceinline__ int value_piece(int d, int piece) { return d * (kWideKeys / 8) + (piece ^ ((d ^ (d >> 3)) & 7)); }
+    static __device__ __forceinline__ int value_piece(int d, int piece) { return d * (kWideKeys / 8) + (piece ^ (((d >> 1) ^ (d >> 4)) & 7)); }
     __device__ __forceinline__ u32x2 *value_quad(int d, int quad)
     {
         return reinterpret_cast<u32x2 *>(&v[value_piece(d, quad / 4 * 2 + (quad & 1))]) + (quad >> 1 & 1);
@@ -200,7 +201,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
         for (int e = 0; e < 16; ++e) o[m][e] = 0.0f;
 
     // ---- a tile in LDS: scores, softmax, second product.  `sees`: bit j, the lane's row sees key j; looked at if `masked` ----
-    auto work = [&](const Tile<kDim> &in, bool masked, uint64_t sees, auto left_out) {
+    auto work = [&](const Tile<kDim> &in, bool masked, uint64_t sees, auto ask, auto left_out) {
         f32x16 s[2];
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[0][e] = s[1][e] = 0.0f;
@@ -211,6 +212,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
                 s[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, in.k[Tile<kDim>::key_piece(32 * half + i, 2 * p + g)]),
                                                                   __builtin_bit_cast(bf16x8, q[p]), s[half], 0, 0, 0);
         read_ahead<2 * kSteps>();
+        ask();
         if (masked) {
             const uint64_t own = sees >> (4 * g);
 #pragma unroll
@@ -256,18 +258,19 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
         read_ahead<4 * kBlocks>();
     };
 
-    // The next tile goes to LDS and the one after the next but one is asked for, the keys in front of the scores and the values behind them:
-    // a tile's loads at once are more than a compute unit has misses under way, and the waves would stand in line to issue them.
-    // Behind the last tile it is loaded again, to no use: with a load left out, the wait for the one before could not be told from one
-    // for all loads.
+    // The next tile goes to LDS, and the one two further on is asked for behind the scores, while nothing is read from LDS: reads from LDS wait in
+    // line behind loads that cannot be issued because of the misses under way (25 tokens over 8 x 9999 slots: 142 us with the loads in front
+    // of the scores, 127 behind them; 102 where all loads hit the L2).  Behind the last tile it is loaded again, to no use: with a load left
+    // out, the wait for the one before could not be told from one for all loads.
     auto step_of = [&](auto set, auto other, int tile) {
         const int left = n - (begin + tile) * kWideKeys, ahead = std::min(tile + 3, tiles - 1);
-        store(other, left - kWideKeys);
-        load_keys(other, ahead);
-        if (active)
-            work(buffer[set], left < kWideKeys, left < kWideKeys ? (1ull << left) - 1ull : ~0ull, [&](const bf16x8 *) { load_values(other, ahead); });
-        else
+        auto ask = [&] {
+            load_keys(other, ahead);
             load_values(other, ahead);
+        };
+        store(other, left - kWideKeys);
+        if (active) work(buffer[set], left < kWideKeys, left < kWideKeys ? (1ull << left) - 1ull : ~0ull, ask, [](const bf16x8 *) {});
+        else ask();
         look_up(std::min(tile + 4, tiles - 1));
         __syncthreads();
     };
@@ -315,7 +318,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
             }
             if (here < kWideKeys) sees &= (1ull << here) - 1ull;
         }
-        if (active) work(buffer[0], true, sees, [&](const bf16x8 *p) {
+        if (active) work(buffer[0], true, sees, [] {}, [&](const bf16x8 *p) {
             if (not_finite != start) return;
             // elements that were left out, for the rows that see their token (the others must not meet them, not even with a weight
             // of zero)
