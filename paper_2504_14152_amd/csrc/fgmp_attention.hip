@@ -673,12 +673,12 @@ AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t h
     AttendPlan p = {};
     const int64_t groups = (tokens * (q_heads / heads) + 15) / 16;
     int64_t want;   // workgroups that the chip holds at a time
-    if (!f32 && head_dim != 256 && groups > 2) {
-        p.waves_of_rows = groups <= 8 ? 4 : 8;
-        p.row_blocks = (groups + 15) / 16;
-        p.tile_keys = kWideKeys;
-        p.min_tiles = 4;
-        want = p.waves_of_rows == 8 ? 256 : 512;
+    if (!f32 && groups > (head_dim == 256 ? 1 : 2)) {
+        p.waves_of_rows = groups <= 8 || head_dim == 256 ? 4 : 8;
+        p.row_blocks = (groups + 2 * p.waves_of_rows - 1) / (2 * p.waves_of_rows);
+        p.tile_keys = wide_keys((int)head_dim);
+        p.min_tiles = 256 / p.tile_keys;
+        want = p.waves_of_rows == 8 || head_dim == 256 ? 256 : 512;
     } else {
         // as many rows as the registers of a wave hold, in blocks of equal size
         const int64_t most = head_dim == 256 ? 1 : 2;

@@ -66,8 +66,8 @@ __device__ __forceinline__ float logsumexp(float most, float l, float c2)
 // 1 / l; 0 where nothing was seen; NaN stays
 __device__ __forceinline__ float inverse_sum(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }
 
-// BF16, head_dim 64 or 128: 32 rows in each of 4 or 8 waves (fgmp_attention_wide.hip)
-constexpr int kWideKeys = 64;
+// BF16: 32 rows in each of 4 or 8 waves, 4 with head_dim 256 (fgmp_attention_wide.hip)
+constexpr int wide_keys(int head_dim) { return head_dim == 256 ? 32 : 64; }
 void attend_wide(const AttendArgs &a, int waves, uint32_t workgroups, hipStream_t st);
 
 }  // namespace fgmp

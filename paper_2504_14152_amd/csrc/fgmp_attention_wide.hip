@@ -1,5 +1,5 @@
 // Attention of many rows (query heads of a group, for all new tokens): from 33 rows on the waves of a workgroup have rows of their own, 32
-// each, and share the keys and values, which go through LDS in tiles of 64 and are read once for up to 256 rows.
+// each, and share the keys and values, which go through LDS in tiles of 64 (32 where head_dim is 256) and are read once for up to 256 rows (128).
 //
 // The two products of fgmp_attention.hip in 32 x 32 tiles, S^T = K Q^T and O^T += V^T P^T: of a tile of scores lane 32 g + i has row i
 // and keys 8 a + 4 g + j (a, j = 0 .. 3), so the softmax has one step between lanes, and the weights go into the second product from the
@@ -16,14 +16,18 @@ namespace {
 
 template <int kDim>
 struct Tile {
+    static constexpr int kKeys = wide_keys(kDim);
     static constexpr int kPieces = kDim / 8;                       // 16-byte pieces of a key
-    u32x4 k[kWideKeys * kPieces];                                  // [key][piece ^ key]
-    u32x4 v[kDim * kWideKeys / 8];                                 // [element][piece ^ element]
+    u32x4 k[kKeys * kPieces];                                      // [key][piece ^ key]
+    u32x4 v[kDim * kKeys / 8];                                     // [element][piece ^ element]
     // LDS gives 16 lanes 16 bytes each in a cycle: a piece of 16 keys in a row, or of 16 elements, lies in 16 different places of 256 bytes
-    static __device__ __forceinline__ int key_piece(int key, int piece) { return key * kPieces + (piece ^ (kPieces == 16 ? key & 15 : key >> 1 & 7)); }
+    static __device__ __forceinline__ int key_piece(int key, int piece) { return key * kPieces + (piece ^ (kPieces >= 16 ? key & 15 : key >> 1 & 7)); }
     // 16 keys are the k index of a matrix instruction: piece 2 s + g is what lane half g takes of the s-th 16, the groups
     // of four keys 4 s + g and 4 s + g + 2
-    static __device__ __forceinline__ int value_piece(int d, int piece) { return d * (kWideKeys / 8) + (piece ^ (((d >> 1) ^ (d >> 4)) & 7)); }
+    static __device__ __forceinline__ int value_piece(int d, int piece)
+    {
+        return d * (kKeys / 8) + (piece ^ (kKeys == 64 ? ((d >> 1) ^ (d >> 4)) & 7 : ((d >> 2) ^ (d >> 5)) & 3));
+    }
     __device__ __forceinline__ u32x2 *value_quad(int d, int quad)
     {
         return reinterpret_cast<u32x2 *>(&v[value_piece(d, quad / 4 * 2 + (quad & 1))]) + (quad >> 1 & 1);
@@ -59,14 +63,16 @@ __device__ __forceinline__ void read_ahead()
 }
 
 template <int kDim, int kWaves>
-__global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs a)
+__global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_kernel(AttendArgs a)
 {
     typedef float f32x8 __attribute__((ext_vector_type(8)));
+    constexpr int kKeys = wide_keys(kDim), kHalves = kKeys / 32, kGroups = kKeys / 16;   // (of 16 keys: slots of one page)
     constexpr int kThreads = 64 * kWaves, kPieces = kDim / 8, kBlocks = kDim / 32, kSteps = kDim / 16;
     // loads of a thread: kKeyLoads pieces of keys, kKeyRows rows apart; and of values, kRounds times four keys x 2 kWords elements, of which
     // kQuadThreads threads have a row
-    constexpr int kKeyLoads = kWideKeys * kPieces / kThreads, kKeyRows = kThreads / kPieces;
-    constexpr int kWords = kDim / (kWaves == 8 ? 64 : 32), kQuadThreads = kDim / (2 * kWords), kQuads = kThreads / kQuadThreads, kRounds = 16 / kQuads;
+    constexpr int kKeyLoads = kKeys * kPieces / kThreads, kKeyRows = kThreads / kPieces;
+    constexpr int kWords = kWaves == 8 ? kDim / 64 : kDim == 256 ? 4 : kDim / 32, kQuadThreads = kDim / (2 * kWords), kQuads = kThreads / kQuadThreads;
+    constexpr int kRounds = kKeys / 4 / kQuads;
     __shared__ Tile<kDim> buffer[2];
     __shared__ int32_t not_finite;    // the last tile of new tokens some of whose values are not finite
 
@@ -97,7 +103,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
     const int key_group = wave * (64 / kPieces), value_group = wave * (64 / kQuadThreads);   // (in rows, and in quads)
     const uint32_t last_group = (uint32_t)(n - 1) / 16u;     // (used where there are slots)
     auto look_up = [&](int tile) {
-        const uint32_t u = (uint32_t)(begin + tile) * 4u;
+        const uint32_t u = (uint32_t)(begin + tile) * kGroups;
 #pragma unroll
         for (int c = 0; c < kKeyLoads; ++c)
             key_page[c] = a.c.page_of(b, a.c.entry_of(std::min(u + (key_group + c * kKeyRows) / 16, last_group), &key_first[c]));
@@ -121,21 +127,21 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
     };
     // rows behind the last slot in use are read as that one
     auto load_keys = [&](auto set, int tile) {
-        const int left = n - (begin + tile) * kWideKeys;
+        const int left = n - (begin + tile) * kKeys;
 #pragma unroll
         for (int c = 0; c < kKeyLoads; ++c) {
             const char *base = a.c.k + a.c.offset(key_page[c], key_first[c], h);
             int r = (key_row + c * kKeyRows) % 16;
-            if (left < kWideKeys && (key_group + c * kKeyRows) / 16 >= (left - 1) / 16) r = std::min(r, (n - 1) & 15);
+            if (left < kKeys && (key_group + c * kKeyRows) / 16 >= (left - 1) / 16) r = std::min(r, (n - 1) & 15);
             key[set][c] = *reinterpret_cast<const u32x4 *>(base + ((uint32_t)r * step + (uint32_t)key_at));
         }
     };
     auto load_values = [&](auto set, int tile) {
-        const int left = n - (begin + tile) * kWideKeys;
+        const int left = n - (begin + tile) * kKeys;
 #pragma unroll
         for (int round = 0; round < kRounds; ++round) {
             const char *base = a.c.v + a.c.offset(value_page[round], value_first[round], h);
-            const bool last = left < kWideKeys && (value_group + round * kQuads) / 4 >= (left - 1) / 16;
+            const bool last = left < kKeys && (value_group + round * kQuads) / 4 >= (left - 1) / 16;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 int r = (quad + round * kQuads) % 4 * 4 + j;
@@ -162,7 +168,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             const int at = quad + r * kQuads;
-            if (left < kWideKeys) {
+            if (left < kKeys) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -202,28 +208,30 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
 
     // ---- a tile in LDS: scores, softmax, second product.  `sees`: bit j, the lane's row sees key j; looked at if `masked` ----
     auto work = [&](const Tile<kDim> &in, bool masked, uint64_t sees, auto ask, auto left_out) {
-        f32x16 s[2];
+        f32x16 s[kHalves];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[0][e] = s[1][e] = 0.0f;
+        for (int half = 0; half < kHalves; ++half)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[half][e] = 0.0f;
 #pragma unroll
         for (int p = 0; p < kSteps; ++p)
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int half = 0; half < kHalves; ++half)
                 s[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, in.k[Tile<kDim>::key_piece(32 * half + i, 2 * p + g)]),
                                                                   __builtin_bit_cast(bf16x8, q[p]), s[half], 0, 0, 0);
-        read_ahead<2 * kSteps>();
+        read_ahead<kHalves * kSteps>();
         ask();
         if (masked) {
             const uint64_t own = sees >> (4 * g);
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int half = 0; half < kHalves; ++half)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if ((own >> (32 * half + e / 4 * 8 + e % 4) & 1ull) == 0ull) s[half][e] = -INFINITY;
         }
         float top = most;
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int half = 0; half < kHalves; ++half)
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = __builtin_amdgcn_fmed3f(top, s[half][e], INFINITY);   // (a maximum that passes NaN over)
         top = halves_max(top);
@@ -239,9 +247,9 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
                 for (int e = 0; e < 16; ++e) o[m][e] *= alpha;
         }
         const float base = most == -INFINITY ? 0.0f : most * a.c2;
-        bf16x8 p[4];
+        bf16x8 p[kGroups];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < kGroups; ++k) {
             f32x8 w;
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k / 2][k % 2 * 8 + e], a.c2, -base));
@@ -250,12 +258,12 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
         }
         left_out(p);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < kGroups; ++k)
 #pragma unroll
             for (int m = 0; m < kBlocks; ++m)
                 o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, in.v[Tile<kDim>::value_piece(32 * m + i, 2 * k + g)]), p[k], o[m],
                                                                0, 0, 0);
-        read_ahead<4 * kBlocks>();
+        read_ahead<kGroups * kBlocks>();
     };
 
     // The next tile goes to LDS, and the one two further on is asked for behind the scores, while nothing is read from LDS: reads from LDS wait in
@@ -263,19 +271,19 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
     // of the scores, 127 behind them; 102 where all loads hit the L2).  Behind the last tile it is loaded again, to no use: with a load left
     // out, the wait for the one before could not be told from one for all loads.
     auto step_of = [&](auto set, auto other, int tile) {
-        const int left = n - (begin + tile) * kWideKeys, ahead = std::min(tile + 3, tiles - 1);
+        const int left = n - (begin + tile) * kKeys, ahead = std::min(tile + 3, tiles - 1);
         auto ask = [&] {
             load_keys(other, ahead);
             load_values(other, ahead);
         };
-        store(other, left - kWideKeys);
-        if (active) work(buffer[set], left < kWideKeys, left < kWideKeys ? (1ull << left) - 1ull : ~0ull, ask, [](const bf16x8 *) {});
+        store(other, left - kKeys);
+        if (active) work(buffer[set], left < kKeys, left < kKeys ? (1ull << left) - 1ull : ~0ull, ask, [](const bf16x8 *) {});
         else ask();
         look_up(std::min(tile + 4, tiles - 1));
         __syncthreads();
     };
     if (tiles > 0) {
-        store(even, n - begin * kWideKeys);
+        store(even, n - begin * kKeys);
         // (the wait for the queries is here, not at their use in the loop, where it would be one for the tiles on their way, too)
 #pragma unroll
         for (int p = 0; p < kSteps; ++p) asm volatile("" : "+v"(q[p]));
@@ -292,8 +300,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
         if (tile < tiles) step_of(even, odd, tile);
     }
     __syncthreads();
-    for (int start = 0; start < drafted; start += kWideKeys) {
-        const int here = std::min(kWideKeys, drafted - start);
+    for (int start = 0; start < drafted; start += kKeys) {
+        const int here = std::min(kKeys, drafted - start);
         load_new(start);
         bool fine = true;
 #pragma unroll
@@ -311,12 +319,12 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
         uint64_t sees = 0ull;
         if (t < count) {
             if (a.tree != nullptr) {
-                sees = a.tree[((int64_t)b * a.tokens + t) * a.words + (start >> 6)];
+                sees = a.tree[((int64_t)b * a.tokens + t) * a.words + (start >> 6)] >> (start & 63);
             } else {
                 const int upto = t - start;
                 sees = upto >= 63 ? ~0ull : upto < 0 ? 0ull : (2ull << upto) - 1ull;
             }
-            if (here < kWideKeys) sees &= (1ull << here) - 1ull;
+            if (here < 64) sees &= (1ull << here) - 1ull;
         }
         if (active) work(buffer[0], true, sees, [] {}, [&](const bf16x8 *p) {
             if (not_finite != start) return;
@@ -326,7 +334,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attend_wide_kernel(AttendArgs 
                 // key j: element 4 (j / 8) + j % 4 of lane half (j / 4) & 1
                 float own = 0.0f;
 #pragma unroll
-                for (int x = 0; x < 32; ++x)
+                for (int x = 0; x < kKeys / 2; ++x)
                     if (x == j / 8 * 4 + j % 4) own = (float)p[x / 8][x % 8];
                 const float w = __shfl(own, (j >> 2 & 1) * 32 + i);
                 if ((sees >> j & 1ull) == 0ull) continue;
@@ -379,7 +387,9 @@ template <int kDim>
 void launch(const AttendArgs &a, int waves, const dim3 grid, hipStream_t st)
 {
     if (waves == 4) attend_wide_kernel<kDim, 4><<<grid, 256, 0, st>>>(a);
-    else attend_wide_kernel<kDim, 8><<<grid, 512, 0, st>>>(a);
+    if constexpr (kDim != 256) {
+        if (waves == 8) attend_wide_kernel<kDim, 8><<<grid, 512, 0, st>>>(a);
+    }
 }
 
 }  // namespace
@@ -387,7 +397,8 @@ void launch(const AttendArgs &a, int waves, const dim3 grid, hipStream_t st)
 void attend_wide(const AttendArgs &a, int waves, uint32_t workgroups, hipStream_t st)
 {
     if (a.c.head_dim == 64) launch<64>(a, waves, dim3(workgroups), st);
-    else launch<128>(a, waves, dim3(workgroups), st);
+    else if (a.c.head_dim == 128) launch<128>(a, waves, dim3(workgroups), st);
+    else launch<256>(a, waves, dim3(workgroups), st);
 }
 
 }  // namespace fgmp

@@ -157,6 +157,9 @@ ATTEND = [
     (BF16, 128, 4, 1, 9, [0, 127, 128], 80, True, [9, 0, 5]),
     (BF16, 128, 12, 2, 10, [1000], 64, False, None),
     (BF16, 128, 24, 2, 12, [2049, 511], 32, True, [12, 7]),
+    (BF16, 256, 8, 1, 5, [333, 31, 0], 32, True, [5, 3, 4]),
+    (BF16, 256, 24, 2, 13, [700, 32], 16, False, [13, 9]),
+    (BF16, 256, 2, 2, 70, [33, 129], 48, True, [70, 65]),
     (F32, 64, 4, 4, 1, [1, 700], 0, False, None),
     (F32, 128, 8, 2, 4, [0, 15, 16, 17], 16, True, [4, 4, 0, 3]),
     (F32, 256, 2, 1, 7, [123], 48, True, None),
@@ -187,7 +190,7 @@ def test_attention_against_its_formula(dtype, D, H, G, T, lens, page, tree, coun
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-@pytest.mark.parametrize("H,G,D", [(4, 2, 64), (1, 1, 64), (3, 1, 128), (10, 2, 128), (12, 1, 64)])
+@pytest.mark.parametrize("H,G,D", [(4, 2, 64), (1, 1, 64), (3, 1, 128), (10, 2, 128), (12, 1, 64), (4, 2, 256)])
 def test_hidden_tokens_reach_no_row_whatever_they_hold(H, G, D, dtype, bad):
     """A new token whose key and value are not finite, seen by some rows and not by others: the others' results are as if it
     were not there; those that see it get no finite result."""
