@@ -677,7 +677,7 @@ AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t h
         p.waves_of_rows = groups <= 8 || head_dim == 256 ? 4 : 8;
         p.row_blocks = (groups + 2 * p.waves_of_rows - 1) / (2 * p.waves_of_rows);
         p.tile_keys = wide_keys((int)head_dim);
-        p.min_tiles = 256 / p.tile_keys;
+        p.min_tiles = 128 / p.tile_keys;
         want = p.waves_of_rows == 8 || head_dim == 256 ? 256 : 512;
     } else {
         // as many rows as the registers of a wave hold, in blocks of equal size
