@@ -618,7 +618,11 @@ __global__ void __launch_bounds__(64 * kWaves) weights_kernel(WeightArgs a)
         const int mine = first + wave * 16 * kWeightKeys, next = first + a.blocks * kBlock;
         Operand<kF32, kDim> ahead[kWeightKeys];
         if (next < n) load(next, ahead);
-        float sum[kWeightKeys] = {};
+        // (what the slots have is on its way meanwhile, too)
+        const int64_t at = ((int64_t)b * a.c.heads + h) * a.stride + mine + i;
+        float have[kWeightKeys], sum[kWeightKeys] = {};
+#pragma unroll
+        for (int s = 0; s < kWeightKeys; ++s) have[s] = g == 0 && mine + 16 * s + i < n ? a.weights[at + 16 * s] : 0.0f;
         for (int start = 0; start < rows; start += kStage) {
             if (!once) {
                 __syncthreads();
@@ -647,11 +651,7 @@ __global__ void __launch_bounds__(64 * kWaves) weights_kernel(WeightArgs a)
 #pragma unroll
         for (int s = 0; s < kWeightKeys; ++s) {
             const float total = over_groups_sum(sum[s]);
-            const int slot = mine + 16 * s + i;
-            if (g == 0 && slot < n) {
-                const int64_t at = ((int64_t)b * a.c.heads + h) * a.stride + slot;
-                a.out[at] = a.weights[at] + total;
-            }
+            if (g == 0 && mine + 16 * s + i < n) a.out[at + 16 * s] = have[s] + total;
         }
 #pragma unroll
         for (int s = 0; s < kWeightKeys; ++s) kt[s] = ahead[s];
