@@ -125,19 +125,25 @@ struct RowState {
     f32x4 o[kDim / 16];
 };
 
+// Over the four lanes of a row (lanes apart by 16), the same in all of them: halves of the wave change places, then rows of 16 lanes.
 __device__ __forceinline__ float over_groups_max(float x)
 {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    x = fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+    const auto q = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)q[0]), __builtin_bit_cast(float, (uint32_t)q[1]));
 }
 __device__ __forceinline__ float over_groups_sum(float x)
 {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    x = __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+    const auto q = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return __builtin_bit_cast(float, (uint32_t)q[0]) + __builtin_bit_cast(float, (uint32_t)q[1]);
 }
 
 // The softmax of one tile: s[sub][j] are the lane's scores (masked ones -inf); p: the weights as the operand of the second product,
-// relative to the new maximum, by which the state is scaled.
+// relative to st.m, the maximum until it is exceeded by a
+// factor of 2^kSlack: then the state is scaled to the new one.
 template <bool kF32, int kDim>
 struct Weights;
 template <int kDim>
@@ -152,7 +158,7 @@ __device__ __forceinline__ void weigh(RowState<kDim> &st, const f32x4 *s, Weight
     float most = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
     if constexpr (kSubs == 2) most = fmaxf(most, fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     most = fmaxf(over_groups_max(most), st.m);
-    if (__any(most > st.m)) {
+    if (__any((most - st.m) * c2 > kSlack)) {
         // (-inf - -inf: nothing has been seen yet, whatever factor is applied to zeros)
         const float alpha = st.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((st.m - most) * c2);
         st.m = most;

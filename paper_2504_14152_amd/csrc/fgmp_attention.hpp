@@ -12,6 +12,9 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
+// The maximum only keeps the exponentials in range: results are scaled to a new one when it is 2^kSlack times the old one's weight, not at
+// every small step up, which some row of 32 makes in nearly every tile.
+constexpr float kSlack = 8.0f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttendArgs {

@@ -46,8 +46,6 @@ __device__ __forceinline__ float halves_max(float x)
     return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
 }
 
-constexpr float kSlack = 8.0f;
-
 // In the order of the instructions before it: kN reads from LDS, each for one matrix instruction, run kAhead in front of them.
 template <int kN>
 __device__ __forceinline__ void read_ahead()
@@ -235,8 +233,6 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = __builtin_amdgcn_fmed3f(top, s[half][e], INFINITY);   // (a maximum that passes NaN over)
         top = halves_max(top);
-        // The maximum only keeps the exponentials in range: results are scaled to a new one when it is 2^kSlack times the old one's
-        // weight, not at every small step up, which some row of 32 makes in nearly every tile.
         if (__any((top - most) * a.c2 > kSlack)) {
             const float alpha = most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((most - top) * a.c2);
             most = top;
