@@ -350,7 +350,8 @@ fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, 
  * over the accepted tokens i = 0 .. counts[b] - 1 of sequence b, which are its newest slots (call this after
  * fgmp_cache_append), and the query heads h that share key head g; accepted token i sees the slots up to its own,
  * j <= lengths[b] - counts[b] + i.
- *   q, lse     as fgmp_tree_attention took and gave them, batch x tokens x q_heads
+ *   q, lse     as fgmp_tree_attention took and gave them, batch x tokens x q_heads; a row whose lse is -inf saw nothing and adds
+ *              nothing
  *   rows       nullable (token i is row i); batch x accepted: which of the `tokens` rows the i-th accepted token is; an
  *              entry outside 0 .. tokens - 1 adds nothing
  *   counts     nullable (accepted); per sequence, 0 .. accepted

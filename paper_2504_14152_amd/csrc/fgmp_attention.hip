@@ -601,6 +601,7 @@ __global__ void __launch_bounds__(64 * kWaves) weights_kernel(WeightArgs a)
             if (r < rows) {
                 const int row = a.rows != nullptr ? a.rows[b * (int64_t)a.accepted + t] : t;
                 if ((uint32_t)row < (uint32_t)a.tokens) lse = a.lse[((int64_t)b * a.tokens + row) * a.q_heads + h * a.group + r - t * a.group] * kLog2e;
+                if (lse == -INFINITY) lse = INFINITY;   // (a row that saw nothing has no weights)
             }
             stage_lse[tid] = lse;
             stage_end[tid] = n - count + t + 1;

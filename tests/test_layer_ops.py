@@ -393,6 +393,25 @@ def test_weights_of_a_whole_prompt_without_rows():
         assert bool(((w[b, :, :n].double().sum(-1) - T * H / G).abs() < T * H / G * 1e-5).all())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_token_that_saw_nothing_adds_no_weight(dtype):
+    """Its lse is -inf: e^(s - lse) would be infinite at every slot it is now behind."""
+    g = _gen(10)
+    B, T, H, G, D = 2, 3, 4, 2, 64
+    made = Made(g, [0, 5], G, D, 16, dtype, room=T)
+    q, k, v = _randn(g, B, T, H, D, dtype=dtype), _randn(g, B, T, G, D, dtype=dtype), _randn(g, B, T, G, D, dtype=dtype)
+    words = torch.tensor([[[0], [2], [6]]] * B, dtype=torch.int64, device=DEV)   # (the first token sees no new one)
+    _, lse = fgmp.tree_attention(q, k, v, made.cache, tree=words)
+    assert bool((lse[0, 0] == -math.inf).all()) and bool(torch.isfinite(lse[0, 1:]).all()) and bool(torch.isfinite(lse[1]).all())
+    made.cache.lengths = fgmp.cache_append(k, v, made.cache)
+    made.lens = made.cache.lengths.tolist()
+    made.keys = [made.rows(made.k, b, n) for b, n in enumerate(made.lens)]
+    have = torch.rand(B, G, made.slots, generator=g).to(DEV)
+    got = fgmp.attention_weights(q, lse, made.cache, have, out=torch.empty_like(have))
+    # (row -1 is none)
+    _compare_weights(got, have, made, q, lse, [[-1, 1, 2], [0, 1, 2]], [T, T], D ** -0.5, H // G)
+
+
 # ---- append ----
 
 @pytest.mark.parametrize("source", [BF16, F32])
