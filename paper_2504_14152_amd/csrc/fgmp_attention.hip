@@ -826,6 +826,7 @@ fgmp_status_t fgmp_attention_weights(const fgmp_heads_t *q, const float *lse, in
     const int64_t pairs = (int64_t)a.c.batch * a.c.heads;
     // (about as many workgroups as the chip holds at a time)
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>((max_length + kBlock - 1) / kBlock, (kWeightWorkgroups + pairs - 1) / pairs));
+    if (pairs * blocks >= (int64_t)1 << 31) return FGMP_ERR_UNSUPPORTED;
     a.q = static_cast<const char *>(q->data);
     a.q_batch = q->batch_stride * size, a.q_token = q->token_stride * size, a.q_head = q->head_stride * size;
     a.lse = lse;

@@ -75,6 +75,15 @@ def test_sizes():
     assert ev(2, 8, 1000, 1000) >= 2 * 8 * 4 and ev(2, 8, 1000, 400) >= 2 * 8 * (4 + 8 * 400)
 
 
+def test_more_workgroups_than_a_grid_counts_are_refused():
+    L, many = fgmp.lib(), 65535
+    c = _cache(batch=many, heads=many)
+    assert _attend(cache=c, q_heads=many, ws_n=1 << 62) == UNSUPPORTED
+    assert L.fgmp_attention_weights(_heads(), AT, 2, many, c, None, 2, None, 0.5, 0, AT, AT, 256, None) == UNSUPPORTED
+    assert L.fgmp_cache_append(_heads(), _heads(), 1, 1 << 20, c, None, 1 << 20, None, None, None, None, 0, AT + 64, None) == UNSUPPORTED
+    assert L.fgmp_cache_evict(c, AT, AT, 256, AT, 10, 0, 0, AT, AT, AT + 64, AT, 1 << 62, None) == UNSUPPORTED
+
+
 def test_weights_append_and_evict_refuse():
     L = fgmp.lib()
 
