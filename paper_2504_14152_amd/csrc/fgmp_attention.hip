@@ -158,10 +158,12 @@ __device__ __forceinline__ void weigh(RowState<kDim> &st, const f32x4 *s, Weight
     float most = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
     if constexpr (kSubs == 2) most = fmaxf(most, fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     most = fmaxf(over_groups_max(most), st.m);
-    if (__any((most - st.m) * c2 > kSlack)) {
-        // (-inf - -inf: nothing has been seen yet, whatever factor is applied to zeros)
-        const float alpha = st.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((st.m - most) * c2);
-        st.m = most;
+    // (-inf - -inf is not above it: nothing has been seen yet)
+    const bool above = (most - st.m) * c2 > kSlack;
+    if (__any(above)) {
+        // each row for itself: what a row gets must not depend on the rows it shares a wave with
+        const float alpha = !above ? 1.0f : st.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((st.m - most) * c2);
+        st.m = above ? most : st.m;
         st.l *= alpha;
 #pragma unroll
         for (int m = 0; m < kPer; ++m) st.o[m] *= alpha;

@@ -233,9 +233,11 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = __builtin_amdgcn_fmed3f(top, s[half][e], INFINITY);   // (a maximum that passes NaN over)
         top = halves_max(top);
-        if (__any((top - most) * a.c2 > kSlack)) {
-            const float alpha = most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((most - top) * a.c2);
-            most = top;
+        const bool above = (top - most) * a.c2 > kSlack;
+        if (__any(above)) {
+            // each row for itself: what a row gets must not depend on the rows it shares a wave with
+            const float alpha = !above ? 1.0f : most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((most - top) * a.c2);
+            most = above ? top : most;
             l *= alpha;
 #pragma unroll
             for (int m = 0; m < kBlocks; ++m)

@@ -218,6 +218,32 @@ def test_hidden_tokens_reach_no_row_whatever_they_hold(H, G, D, dtype, bad):
                 assert torch.equal(out[0, t], plain[0, t]) and torch.equal(lse[0, t], plain_lse[0, t])
 
 
+@pytest.mark.parametrize("dtype,H,G,D,T", [(BF16, 4, 2, 64, 7), (BF16, 3, 1, 128, 9), (BF16, 8, 2, 128, 20), (BF16, 16, 1, 64, 30), (BF16, 10, 1, 128, 20),
+                                           (BF16, 2, 2, 256, 13), (BF16, 8, 1, 256, 25), (F32, 4, 2, 128, 14), (F32, 2, 1, 256, 8)])
+def test_no_row_depends_on_what_others_score(dtype, H, G, D, T):
+    """Rows share tiles and waves, and nothing else: bit for bit the same results whether other rows' scores are small or large, be it the
+    query of a token that does not count or the key of one that the row does not see."""
+    g = _gen(14)
+    made = Made(g, [1500], G, D, 16, dtype)
+    q, k, v = _randn(g, 1, T, H, D, dtype=dtype), _randn(g, 1, T, G, D, dtype=dtype), _randn(g, 1, T, G, D, dtype=dtype)
+    words, sees = _random_tree(g, 1, T)
+    count = T - 2
+    hidden = min((t for t in range(count) if any(t not in sees[0][u] for u in range(count))), key=lambda t: abs(sum(t in s for s in sees[0][:count]) - count / 2))
+    blind = [t for t in range(count) if hidden not in sees[0][t]]
+    for hint in (0, 1):     # in several ranges, and in one
+        plain, plain_lse = fgmp.tree_attention(q, k, v, made.cache, tree=words, counts=_i32([count]), max_length=hint)
+        loud = q.clone()
+        loud[:, count:] *= 300.0
+        out, lse = fgmp.tree_attention(loud, k, v, made.cache, tree=words, counts=_i32([count]), max_length=hint)
+        _say("queries that do not count", dtype, D, hint, int((out != plain).sum()))
+        assert torch.equal(out, plain) and torch.equal(lse, plain_lse)
+        loud = k.clone()
+        loud[:, hidden] *= 300.0
+        out, lse = fgmp.tree_attention(q, loud, v, made.cache, tree=words, counts=_i32([count]), max_length=hint)
+        _say("a key not seen", dtype, D, hint, int((out[:, blind] != plain[:, blind]).sum()))
+        assert torch.equal(out[:, blind], plain[:, blind]) and torch.equal(lse[:, blind], plain_lse[:, blind])
+
+
 def test_a_token_may_see_nothing_at_all():
     g = _gen(4)
     made = Made(g, [0, 3], 2, 128, 16, BF16)
