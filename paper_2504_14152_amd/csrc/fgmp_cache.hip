@@ -465,11 +465,13 @@ fgmp_status_t fgmp_cache_evict(const fgmp_cache_t *cache, const float *weights, 
     const int piece_shift = log2_of(a.c.head_dim * dtype_size(cache->dtype) / 16);
     const int64_t steps = (a.room + (256 >> piece_shift) - 1) / (256 >> piece_shift);
     const int64_t per_head = std::max<int64_t>(1, std::min<int64_t>(steps, std::max<int64_t>(1, 4096 / pairs)));
-    if (pairs * per_head >= (int64_t)1 << 31) return FGMP_ERR_UNSUPPORTED;
+    if (!launch_counts(pairs, a.c.slots <= 2048 ? 512 : 1024) || !launch_counts(pairs * per_head, 256)) return FGMP_ERR_UNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (a.c.slots <= 2048) evict_select_kernel<512, 1><<<dim3((unsigned)pairs), 512, 0, st>>>(a);
     else if (a.c.slots <= 8192) evict_select_kernel<1024, 2><<<dim3((unsigned)pairs), 1024, 0, st>>>(a);
     else evict_select_kernel<1024, 4><<<dim3((unsigned)pairs), 1024, 0, st>>>(a);
+    // (the moves are read from the workspace: not without the launch that writes them)
+    if (launched() != FGMP_OK) return FGMP_ERR_HIP;
     if (a.room > 0) evict_move_kernel<<<dim3((unsigned)(pairs * per_head)), 256, 0, st>>>(a, (int)per_head, piece_shift);
     return launched();
 }

@@ -53,6 +53,9 @@ struct CacheView {
     }
 };
 
+// A launch counts its threads in 32 bits, not its workgroups: one of more does not take place.
+inline bool launch_counts(int64_t workgroups, int64_t threads) { return workgroups < ((int64_t)1 << 32) / threads; }
+
 inline int dtype_size(fgmp_dtype_t dt) { return dt == FGMP_F32 ? 4 : 2; }
 inline bool known_dtype(fgmp_dtype_t dt) { return dt == FGMP_F32 || dt == FGMP_BF16; }
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0u; }

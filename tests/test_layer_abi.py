@@ -84,6 +84,15 @@ def test_more_workgroups_than_a_grid_counts_are_refused():
     assert L.fgmp_cache_evict(c, AT, AT, 256, AT, 10, 0, 0, AT, AT, AT + 64, AT, 1 << 62, None) == UNSUPPORTED
 
 
+@pytest.mark.parametrize("slots,heads", [(64, 129), (2048, 129), (4096, 65), (16384, 65)])
+def test_an_eviction_of_more_threads_than_a_launch_counts_is_refused(slots, heads):
+    """A launch counts its threads in 32 bits: 512 for a sequence and head up to 2048 slots, 1024 above.  The launch that moves has fewer: it
+    must not run over moves that the one before it has not written."""
+    c = _cache(batch=65535, heads=heads, pages_per_sequence=slots // 64, table_stride=slots // 64)
+    assert 65535 * (heads - 1) * (512 if slots <= 2048 else 1024) < 1 << 32 <= 65535 * heads * (512 if slots <= 2048 else 1024)
+    assert fgmp.lib().fgmp_cache_evict(c, AT, AT, slots, AT, 10, 0, 0, AT, AT, AT + 64, AT, 1 << 62, None) == UNSUPPORTED
+
+
 def test_weights_append_and_evict_refuse():
     L = fgmp.lib()
 
