@@ -770,7 +770,8 @@ fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, 
         if (!aligned16(workspace)) return FGMP_ERR_BAD_ALIGN;
         if (workspace_bytes < need) return FGMP_ERR_BUFFER_TOO_SMALL;
     }
-    if (p.workgroups >= (int64_t)1 << 31 || rows >= (int64_t)1 << 31) return FGMP_ERR_UNSUPPORTED;
+    // (ranges are joined only where heads and row blocks are fewer than 1024, of 256 rows at most: that launch stays small)
+    if (!launch_counts(p.workgroups, 64 * (p.waves_of_rows > 0 ? p.waves_of_rows : kWaves)) || rows >= (int64_t)1 << 31) return FGMP_ERR_UNSUPPORTED;
     a.q = static_cast<const char *>(q->data);
     a.q_batch = q->batch_stride * size, a.q_token = q->token_stride * size, a.q_head = q->head_stride * size;
     a.out = static_cast<char *>(out->data);
@@ -828,7 +829,7 @@ fgmp_status_t fgmp_attention_weights(const fgmp_heads_t *q, const float *lse, in
     const int64_t pairs = (int64_t)a.c.batch * a.c.heads;
     // (about as many workgroups as the chip holds at a time)
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>((max_length + kBlock - 1) / kBlock, (kWeightWorkgroups + pairs - 1) / pairs));
-    if (pairs * blocks >= (int64_t)1 << 31) return FGMP_ERR_UNSUPPORTED;
+    if (!launch_counts(pairs * blocks, 64 * kWaves)) return FGMP_ERR_UNSUPPORTED;
     a.q = static_cast<const char *>(q->data);
     a.q_batch = q->batch_stride * size, a.q_token = q->token_stride * size, a.q_head = q->head_stride * size;
     a.lse = lse;

@@ -404,7 +404,7 @@ fgmp_status_t fgmp_cache_append(const fgmp_heads_t *k, const fgmp_heads_t *v, fg
     const int per_head = a.c.head_dim * dtype_size(cache->dtype) / 16;
     const int64_t pieces = (int64_t)a.c.heads * per_head;
     const int64_t per_token = std::max<int64_t>(1, std::min<int64_t>((pieces + 255) / 256, 64));
-    if (tokens > (int64_t)1 << 30 || accepted > (int64_t)1 << 30 || a.c.batch * accepted * per_token >= (int64_t)1 << 31) return FGMP_ERR_UNSUPPORTED;
+    if (tokens > (int64_t)1 << 30 || accepted > (int64_t)1 << 30 || !launch_counts(a.c.batch * accepted * per_token, 256)) return FGMP_ERR_UNSUPPORTED;
     a.in = {static_cast<const char *>(k->data), static_cast<const char *>(v->data), k->batch_stride * size, k->token_stride * size,
             k->head_stride * size, v->batch_stride * size, v->token_stride * size, v->head_stride * size};
     a.tokens = tokens;

@@ -148,27 +148,30 @@ __global__ void __launch_bounds__(kThreads < 256 ? 256 : kThreads) norm_kernel(N
 }
 
 template <bool kXF32, bool kOF32, bool kHF32, int kThreads, int kChunks>
-void norm_launch(const NormArgs &a, hipStream_t st)
+fgmp_status_t norm_launch(const NormArgs &a, hipStream_t st)
 {
     constexpr int kRows = kThreads < 256 ? 256 / kThreads : 1;
-    norm_kernel<kXF32, kOF32, kHF32, kThreads, kChunks><<<dim3((unsigned)((a.M + kRows - 1) / kRows)), kThreads * kRows, 0, st>>>(a);
+    const int64_t workgroups = (a.M + kRows - 1) / kRows;
+    if (!launch_counts(workgroups, kThreads * kRows)) return FGMP_ERR_UNSUPPORTED;
+    norm_kernel<kXF32, kOF32, kHF32, kThreads, kChunks><<<dim3((unsigned)workgroups), kThreads * kRows, 0, st>>>(a);
+    return hipGetLastError() == hipSuccess ? FGMP_OK : FGMP_ERR_HIP;
 }
 
 // Threads of a row by its width: 64 M elements, residual stream and h in BF16, o in FP32, at 5.3 to 5.8 TB/s from 128 columns to 16384 (4.1 at
 // 64, 4.3 above).  With a workgroup to every row 64 columns ran at 0.5 TB/s and 512 at 3.3; with 512 threads holding 32 elements each
 // 11008 and 16384 columns at 3.7 and 4.0.
 template <bool kXF32, bool kOF32, bool kHF32>
-void norm_launch_width(const NormArgs &a, hipStream_t st)
+fgmp_status_t norm_launch_width(const NormArgs &a, hipStream_t st)
 {
-    if (a.K <= 128) norm_launch<kXF32, kOF32, kHF32, 16, 1>(a, st);
-    else if (a.K <= 256) norm_launch<kXF32, kOF32, kHF32, 32, 1>(a, st);
-    else if (a.K <= 512) norm_launch<kXF32, kOF32, kHF32, 64, 1>(a, st);
-    else if (a.K <= 1024) norm_launch<kXF32, kOF32, kHF32, 64, 2>(a, st);
-    else if (a.K <= 2048) norm_launch<kXF32, kOF32, kHF32, 256, 1>(a, st);
-    else if (a.K <= 4096) norm_launch<kXF32, kOF32, kHF32, 256, 2>(a, st);
-    else if (a.K <= 8192) norm_launch<kXF32, kOF32, kHF32, 512, 2>(a, st);
-    else if (a.K <= 16384) norm_launch<kXF32, kOF32, kHF32, 1024, 2>(a, st);
-    else norm_launch<kXF32, kOF32, kHF32, 1024, 4>(a, st);
+    if (a.K <= 128) return norm_launch<kXF32, kOF32, kHF32, 16, 1>(a, st);
+    if (a.K <= 256) return norm_launch<kXF32, kOF32, kHF32, 32, 1>(a, st);
+    if (a.K <= 512) return norm_launch<kXF32, kOF32, kHF32, 64, 1>(a, st);
+    if (a.K <= 1024) return norm_launch<kXF32, kOF32, kHF32, 64, 2>(a, st);
+    if (a.K <= 2048) return norm_launch<kXF32, kOF32, kHF32, 256, 1>(a, st);
+    if (a.K <= 4096) return norm_launch<kXF32, kOF32, kHF32, 256, 2>(a, st);
+    if (a.K <= 8192) return norm_launch<kXF32, kOF32, kHF32, 512, 2>(a, st);
+    if (a.K <= 16384) return norm_launch<kXF32, kOF32, kHF32, 1024, 2>(a, st);
+    return norm_launch<kXF32, kOF32, kHF32, 1024, 4>(a, st);
 }
 
 // a row of K elements of type `dt` for each of M rows
@@ -239,14 +242,13 @@ extern "C" fgmp_status_t fgmp_block_norm(const void *x, fgmp_dtype_t x_dt, int64
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int types = (x_dt == FGMP_F32 ? 4 : 0) + (o != nullptr && o_dt == FGMP_F32 ? 2 : 0) + (h != nullptr && h_dt == FGMP_F32 ? 1 : 0);
     switch (types) {
-    case 0: norm_launch_width<false, false, false>(a, st); break;
-    case 1: norm_launch_width<false, false, true>(a, st); break;
-    case 2: norm_launch_width<false, true, false>(a, st); break;
-    case 3: norm_launch_width<false, true, true>(a, st); break;
-    case 4: norm_launch_width<true, false, false>(a, st); break;
-    case 5: norm_launch_width<true, false, true>(a, st); break;
-    case 6: norm_launch_width<true, true, false>(a, st); break;
-    default: norm_launch_width<true, true, true>(a, st); break;
+    case 0: return norm_launch_width<false, false, false>(a, st);
+    case 1: return norm_launch_width<false, false, true>(a, st);
+    case 2: return norm_launch_width<false, true, false>(a, st);
+    case 3: return norm_launch_width<false, true, true>(a, st);
+    case 4: return norm_launch_width<true, false, false>(a, st);
+    case 5: return norm_launch_width<true, false, true>(a, st);
+    case 6: return norm_launch_width<true, true, false>(a, st);
+    default: return norm_launch_width<true, true, true>(a, st);
     }
-    return hipGetLastError() == hipSuccess ? FGMP_OK : FGMP_ERR_HIP;
 }

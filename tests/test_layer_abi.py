@@ -93,6 +93,27 @@ def test_an_eviction_of_more_threads_than_a_launch_counts_is_refused(slots, head
     assert fgmp.lib().fgmp_cache_evict(c, AT, AT, slots, AT, 10, 0, 0, AT, AT, AT + 64, AT, 1 << 62, None) == UNSUPPORTED
 
 
+def test_more_threads_than_a_launch_counts_are_refused():
+    """2^32 threads, in workgroups of 256 or 512, are too many: each call just past that."""
+    L, many = fgmp.lib(), 65535
+    # attention: one workgroup of 256 for each head of a sequence, 512 where a head has more than 128 rows
+    assert _attend(cache=_cache(batch=many, heads=257), tokens=1, q_heads=257, max_length=1) == UNSUPPORTED
+    wide = _cache(batch=many, heads=129)
+    assert _attend(cache=wide, tokens=129, q_heads=129, max_length=1, q=_heads(strides=(1 << 16, 128, 1 << 12)), out=_heads(strides=(1 << 16, 128, 1 << 12)),
+                   k=_heads(strides=(1 << 16, 128, 1 << 12)), v=_heads(strides=(1 << 16, 128, 1 << 12))) == UNSUPPORTED
+    # weights: at least one workgroup of 256 for each head of a sequence
+    assert L.fgmp_attention_weights(_heads(), AT, 2, 257, _cache(batch=many, heads=257), None, 2, None, 0.5, 0, AT, AT, 256, None) == UNSUPPORTED
+    # append: one of 256 for each token of up to 16 heads
+    assert L.fgmp_cache_append(_heads(), _heads(), 1, 257, _cache(batch=many), None, 257, None, None, None, None, 0, AT + 64, None) == UNSUPPORTED
+
+    def norm(M, K):
+        return L.fgmp_block_norm(AT, 1, K, None, 1, 0, None, 0, 1, 0, M, K, None, None, AT, None, 0, 1e-5, 1.0, 1.0, None, 0, AT, 1, K, None)
+
+    # norms: as many threads as a row has
+    for K, threads in [(64, 16), (128, 16), (144, 32), (512, 64), (1024, 64), (2048, 256), (4096, 256), (8192, 512), (16384, 1024), (32768, 1024)]:
+        assert norm((1 << 32) // threads, K) == UNSUPPORTED, K
+
+
 def test_weights_append_and_evict_refuse():
     L = fgmp.lib()
 
