@@ -19,6 +19,7 @@ from . import listing_check
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfgmp.so")
+HEADER = os.path.join(os.path.dirname(HERE), "include", "fgmp.h")
 CALL_SOURCE = os.path.join(CSRC, "fgmp_call.c")
 # what the binding hands the fused call's arguments over with; the name says for which interpreter
 CALL = os.path.join(HERE, "_fgmp_call" + sysconfig.get_config_var("EXT_SUFFIX"))
@@ -39,8 +40,7 @@ def lib_path(variant: str | None = None) -> str:
 def source_files() -> list[str]:
     """Every file a library is built from (for the staleness check of the binding)."""
     files = [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith((".hip", ".hpp"))]
-    files.append(os.path.join(os.path.dirname(HERE), "include", "fgmp.h"))
-    return files
+    return files + [HEADER]
 
 
 def is_stale(path: str) -> bool:
@@ -48,6 +48,11 @@ def is_stale(path: str) -> bool:
         return True
     t = os.path.getmtime(path)
     return any(os.path.getmtime(f) > t for f in source_files())
+
+
+def call_is_stale() -> bool:
+    """The extension module is compiled with the header, too: argument lists, structures and codes are its."""
+    return not os.path.exists(CALL) or any(os.path.getmtime(f) > os.path.getmtime(CALL) for f in (CALL_SOURCE, HEADER))
 
 
 def _hipcc() -> str:

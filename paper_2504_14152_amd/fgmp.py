@@ -78,12 +78,12 @@ def lib() -> ctypes.CDLL:
 
 @functools.cache
 def _load_call():
-    """The extension module that passes the fused call's arguments on, built from its source where it is missing or older.  None
+    """The extension module that passes the fused call's arguments on, built from its sources where it is missing or older.  None
     where it cannot be built or loaded (no compiler, no Python headers, a folder that is not written to): it saves host time only,
     and ctypes calls the same entry point."""
     try:
         path = _build.CALL
-        if not os.path.exists(path) or os.path.getmtime(path) < os.path.getmtime(_build.CALL_SOURCE):
+        if _build.call_is_stale():
             _build.build_call()
         loader = importlib.machinery.ExtensionFileLoader("_fgmp_call", path)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_fgmp_call", loader))

@@ -274,6 +274,41 @@ def test_the_extension_is_this_interpreters_and_appears_whole(tmp_path, monkeypa
     assert (tmp_path / "module.so.seen").read_text() == "before" and sorted(os.listdir(tmp_path)) == ["cc", "module.so", "module.so.seen"]
 
 
+@pytest.mark.parametrize("compiles", [True, False])
+def test_the_extension_is_built_again_behind_its_header(tmp_path, monkeypatch, compiles):
+    """It calls entry points with the argument lists and structures of fgmp.h as it was compiled with: a module older than the header is
+    built again, as one older than its own source is, and not loaded where that fails."""
+    import shutil
+    fgmp.lib()
+    place, source, header = tmp_path / "module.so", tmp_path / "source.c", os.path.join(os.path.dirname(build.HERE), "include", "fgmp.h")
+    shutil.copy(build.CALL, place)
+    source.write_text("")
+    t = os.path.getmtime(header)
+    os.utime(source, (t - 20, t - 20))
+    os.utime(place, (t - 10, t - 10))
+    built = []
+
+    def build_call():
+        built.append(1)
+        if not compiles:
+            raise RuntimeError("no compiler")
+        os.utime(place, (t + 10, t + 10))
+        return str(place)
+
+    monkeypatch.setattr(build, "CALL", str(place))
+    monkeypatch.setattr(build, "CALL_SOURCE", str(source))
+    monkeypatch.setattr(build, "build_call", build_call)
+    fgmp._load_call.cache_clear()
+    try:
+        module = fgmp._load_call()
+        assert built == [1] and (module is not None) == compiles
+        if compiles:      # one that is newer than both is taken as it is
+            fgmp._load_call.cache_clear()
+            assert fgmp._load_call() is not None and built == [1]
+    finally:
+        fgmp._load_call.cache_clear()
+
+
 @pytest.mark.parametrize("what", ["X.is_cuda", "X.shape", "X.dtype", "X.data_ptr", "X.stride", "fisher.is_cuda", "fisher.data_ptr", "w.K", "w.rows",
                                   "w.buf.data_ptr", "out.data_ptr", "out.stride", "workspace.data_ptr", "workspace.numel"])
 def test_the_extension_asks_nothing_more_once_something_failed(what):
