@@ -354,7 +354,8 @@ fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, 
  *              nothing
  *   rows       nullable (token i is row i); batch x accepted: which of the `tokens` rows the i-th accepted token is; an
  *              entry outside 0 .. tokens - 1 adds nothing
- *   counts     nullable (accepted); per sequence, 0 .. accepted
+ *   counts     nullable (accepted); per sequence, 0 .. accepted: the tokens that have a slot.  Where fgmp_cache_append had no slots
+ *              for some, that is the difference of its lengths_out and the lengths before it, not the counts it was given
  *   weights, out  batch x cache->heads rows of `weights_stride` FP32 elements, one per slot; the same array, or arrays that do
  *              not overlap.  Entries of slots not in use are neither read nor written.
  */
@@ -370,8 +371,10 @@ fgmp_status_t fgmp_attention_weights(const fgmp_heads_t *q, const float *lse, in
  *   positions  nullable; batch x tokens: a token's position in its sequence
  *   slot_positions, slot_weights   nullable; batch x cache->heads rows of `slot_stride` elements: the new slots get
  *              the token's position (needs `positions`) and weight 0
- *   lengths_out  one per sequence: lengths[b] + counts[b]; an array of its own, not cache->lengths
- * Tokens for which a sequence has no slots left are dropped.
+ *   lengths_out  one per sequence: lengths[b] + counts[b], but no more than the sequence has slots; an array of its own, not
+ *              cache->lengths
+ * Tokens for which a sequence has no slots left are dropped: lengths_out - lengths are the counts of those that were stored, which is
+ * what fgmp_attention_weights has to be given then.
  */
 fgmp_status_t fgmp_cache_append(const fgmp_heads_t *k, const fgmp_heads_t *v, fgmp_dtype_t dt, int64_t tokens,
                                 const fgmp_cache_t *cache, const int32_t *rows, int64_t accepted, const int32_t *counts,

@@ -693,7 +693,7 @@ def attention_weights(q: torch.Tensor, lse: torch.Tensor, cache: Cache, weights:
                       counts: torch.Tensor | None = None, scale: float | None = None, max_length: int = 0, out: torch.Tensor | None = None):
     """`weights` (batch x heads x slots, float32) and what the accepted tokens' attention adds to it, in `out` (`weights` itself unless
     given): call it after cache_append, with the q and lse that tree_attention took and gave.  `rows` (int32, batch x accepted): which
-    rows of q were accepted; `counts` (int32): how many of them."""
+    rows of q were accepted; `counts` (int32): how many of them, and were stored: the growth of the lengths, where the cache may be full."""
     if scale is not None and _handed("attention_weights", q, lse, cache._handle, weights, rows, counts, scale, max_length,
                                      weights if out is None else out):
         return weights if out is None else out
@@ -726,7 +726,8 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, cache: Cache, rows: torch.Ten
                  slot_weights: torch.Tensor | None = None, lengths_out: torch.Tensor | None = None) -> torch.Tensor:
     """Keys and values of accepted tokens (`rows`, `counts` as attention_weights; k, v as tree_attention, float32 too) into the next slots
     of the cache; returns the new lengths, for cache.lengths.  `positions` (int32, batch x tokens) go to `slot_positions` (int32, batch x
-    heads x slots); `slot_weights` (float32) of new slots become 0."""
+    heads x slots); `slot_weights` (float32) of new slots become 0.  Tokens without a slot are dropped: the new lengths less the old ones are the
+    `counts` that were stored."""
     if lengths_out is not None and _handed("cache_append", k, v, cache._handle, rows, counts, positions, slot_positions, slot_weights, lengths_out):
         return lengths_out
     _require_cuda(k, v, rows, counts, positions, slot_positions, slot_weights, lengths_out)

@@ -486,6 +486,26 @@ def test_append_drops_what_has_no_slot():
     assert torch.equal(made.rows(made.v, 0, 32)[30:], k[0, :2])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_weights_behind_an_append_that_had_no_slots_for_all(dtype):
+    """The growth of the lengths is how many tokens were stored: with that as `counts` each of them sees the slots up to its own, and the
+    tokens that were dropped add nothing."""
+    g = _gen(15)
+    B, T, H, G, D = 3, 4, 4, 2, 64
+    made = Made(g, [30, 32, 27], G, D, 16, dtype)       # 32 slots each: room for 2, 0 and 5
+    q, k, v = _randn(g, B, T, H, D, dtype=dtype), _randn(g, B, T, G, D, dtype=dtype), _randn(g, B, T, G, D, dtype=dtype)
+    _, lse = fgmp.tree_attention(q, k, v, made.cache)
+    old = made.cache.lengths
+    made.cache.lengths = fgmp.cache_append(k, v, made.cache, counts=_i32([4, 4, 3]))
+    stored = made.cache.lengths - old
+    assert stored.tolist() == [2, 0, 3]
+    made.lens = made.cache.lengths.tolist()
+    made.keys = [made.rows(made.k, b, n) for b, n in enumerate(made.lens)]
+    have = torch.rand(B, G, made.slots, generator=g).to(DEV)
+    got = fgmp.attention_weights(q, lse, made.cache, have, counts=stored, out=torch.empty_like(have))
+    _compare_weights(got, have, made, q, lse, [list(range(T))] * B, stored.tolist(), D ** -0.5, H // G)
+
+
 def test_a_page_that_is_none_of_the_cache_is_not_written():
     g = _gen(11)
     made = Made(g, [16], 1, 64, 16, BF16)
