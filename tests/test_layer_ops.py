@@ -244,6 +244,44 @@ def test_no_row_depends_on_what_others_score(dtype, H, G, D, T):
         assert torch.equal(out[:, blind], plain[:, blind]) and torch.equal(lse[:, blind], plain_lse[:, blind])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,G,D", [(4, 2, 64), (1, 1, 64), (3, 1, 128), (10, 2, 128), (12, 1, 64), (4, 2, 256)])
+def test_rows_that_see_a_key_that_is_not_finite_get_what_the_formula_gives(H, G, D, dtype):
+    """A key of NaN: nothing but NaN.  One infinite element: NaN where it makes the score infinite, as if the key were not there where
+    it makes it minus infinity."""
+    g = _gen(16)
+    T = 21
+    made = Made(g, [77], G, D, 16, dtype)
+    q, k, v = _randn(g, 1, T, H, D, dtype=dtype), _randn(g, 1, T, G, D, dtype=dtype), _randn(g, 1, T, G, D, dtype=dtype)
+    q[..., 3] = torch.where(q[..., 3] < 0, -0.5, 0.5)     # (no zeros: their products with infinity are NaN)
+    words, sees = _random_tree(g, 1, T)
+    seen_by = [t for t in range(T) if 9 in sees[0][t]]
+    bad = k.clone()
+    bad[0, 9] = math.nan
+    out, lse = fgmp.tree_attention(q, bad, v, made.cache, tree=words)
+    assert bool(torch.isnan(out[0, seen_by]).all()) and bool(torch.isnan(lse[0, seen_by]).all())
+    bad = k.clone()
+    bad[0, 9, :, 3] = math.inf
+    out, lse = fgmp.tree_attention(q, bad, v, made.cache, tree=words)
+    there = (q[0, :, :, 3] > 0) & torch.tensor([[t in seen_by] for t in range(T)], device=DEV)
+    assert bool(there.any()) and bool((torch.isnan(out[0]).all(-1) == there).all()) and bool((torch.isnan(lse[0]) == there).all())
+    _say("keys that are not finite", dtype, H, G, D, int(there.sum()))
+    # the others by the formula: their token 9 has a weight of zero
+    without = [[[j for j in s if j != 9] for s in sees[0]]]
+    ok = ~there
+    plain, plain_lse = fgmp.tree_attention(q, k, v, made.cache, tree=_words_of(without, T))
+    _compare_attention(torch.where(ok[None, ..., None], out, plain), torch.where(ok[None], lse, plain_lse), q, made, k, v, without, [T], D ** -0.5, H // G)
+
+
+def _words_of(sees, T):
+    words = torch.zeros(len(sees), T, (T + 63) // 64, dtype=torch.int64)
+    for b, rows in enumerate(sees):
+        for t, row in enumerate(rows):
+            for j in row:
+                words[b, t, j // 64] |= (1 << j % 64) - (1 << 64 if j % 64 == 63 else 0)
+    return words.to(DEV)
+
+
 def test_a_token_may_see_nothing_at_all():
     g = _gen(4)
     made = Made(g, [0, 3], 2, 128, 16, BF16)
@@ -329,6 +367,52 @@ def test_offsets_past_32_bits():
         w = fgmp.attention_weights(q, lse, cache, torch.zeros(1, G, 150, device=DEV), counts=_i32([1]))
         assert bool(torch.isfinite(w).all())
         _say("offsets", dtype)
+
+
+@pytest.mark.parametrize("far", ["pages", "rows"])
+def test_all_calls_reach_past_32_bits(far):
+    """More than 32 rows to a key head, tokens appended and entries moved, more than 4 GiB behind the cache's pointers."""
+    g = _gen(17)
+    D, G, H, T, page, n = 128, 2, 4, 40, 64, 150
+    made = Made(g, [n], G, D, 0, BF16)
+    if far == "pages":
+        pages = (5 << 30) // (page * G * D * 2)
+        k, v = (torch.empty(pages, page, G, D, dtype=BF16, device=DEV) for _ in range(2))
+        table = [pages - 1, 0, pages - 7, pages - 3]
+        cache = fgmp.Cache(k, v, _i32([n]), _i32([table]))
+    else:     # (one buffer for both: keys are the values)
+        step, page, table = 1 << 24, 200, [0]
+        k = v = torch.as_strided(torch.empty(200 * step, dtype=BF16, device=DEV), (1, 200, G, D), (200 * step, step, D, 1))
+        made.values[0] = made.keys[0]
+        cache = fgmp.Cache(k, v, _i32([n]))
+
+    def slots(x, count):
+        return torch.cat([x[at] for at in table])[:count].clone()
+
+    for x, rows in ((k, made.keys[0]), (v, made.values[0])):
+        for j in range(0, n, page):
+            x[table[j // page], : min(page, n - j)] = rows[j:j + page]
+    q = _randn(g, 1, T, H, D, dtype=BF16)
+    out, lse = fgmp.tree_attention(q, None, None, cache)
+    _compare_attention(out, lse, q, made, None, None, None, [T], D ** -0.5, H // G)
+    new_k = _randn(g, 1, T, G, D, dtype=BF16)
+    new_v = _randn(g, 1, T, G, D, dtype=BF16) if far == "pages" else new_k
+    positions = torch.arange(n, n + T, dtype=torch.int32, device=DEV)[None]
+    slot_positions = torch.arange(len(table) * page, dtype=torch.int32, device=DEV).repeat(1, G, 1)
+    cache.lengths = fgmp.cache_append(new_k, new_v, cache, positions=positions, slot_positions=slot_positions)
+    old_k, old_v = torch.cat([made.keys[0], new_k[0]]), torch.cat([made.values[0], new_v[0]])
+    assert torch.equal(slots(k, n + T), old_k) and torch.equal(slots(v, n + T), old_v)
+    w = _randn(g, 1, G, len(table) * page).square()
+    w_in = w.clone()
+    budget = 100
+    fgmp.cache_evict(cache, w, slot_positions, _i32([n + T]), budget, 4, 30)
+    got_k, got_v = slots(k, n + T), slots(v, n + T)
+    for h in range(G):
+        now = _evicted(w_in[0, h].tolist(), list(range(n + T)), n + T, n + T, budget, 4, 30)
+        assert any(x != i for i, x in enumerate(now)) and slot_positions[0, h, :budget].tolist() == now
+        assert torch.equal(got_k[:budget, h], old_k[now, h]) and torch.equal(got_v[:budget, h], old_v[now, h])
+        assert torch.equal(got_k[budget:, h], old_k[budget:, h]) and torch.equal(got_v[budget:, h], old_v[budget:, h])
+    _say("offsets of all calls", far)
 
 
 # ---- attention weights ----
