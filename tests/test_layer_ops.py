@@ -188,6 +188,29 @@ def test_attention_against_its_formula(dtype, D, H, G, T, lens, page, tree, coun
     _compare_attention(out, lse, q, made, None, None, None, use, 0.37 * scale, H // G)
 
 
+@pytest.mark.parametrize("dtype,D,H,G,T,lens,page,tree,counts", [
+    (BF16, 128, 2, 1, 1024, [100], 16, False, None),
+    (BF16, 64, 4, 2, 512, [0, 70], 0, True, [512, 300]),
+    (BF16, 256, 1, 1, 600, [33], 48, True, [577]),
+    (BF16, 64, 1, 1, 1023, [2000], 64, False, [1000]),
+    (F32, 64, 2, 1, 1024, [17], 0, False, [1001]),
+    (F32, 128, 1, 1, 515, [0], 16, True, None),
+])
+def test_attention_of_a_chunk_of_a_prompt(dtype, D, H, G, T, lens, page, tree, counts):
+    """Up to as many new tokens as a call takes, over an empty cache and a filled one."""
+    _say("chunk", dtype, D, H, G, T, lens, page, tree, counts)
+    g = _gen(T + D)
+    B = len(lens)
+    made = Made(g, lens, G, D, page, dtype)
+    q, k, v = _randn(g, B, T, H, D, dtype=dtype), _randn(g, B, T, G, D, dtype=dtype), _randn(g, B, T, G, D, dtype=dtype)
+    words, sees = _random_tree(g, B, T) if tree else (None, _chain(B, T))
+    use = [T] * B if counts is None else counts
+    for b in range(B):
+        k[b, use[b]:], v[b, use[b]:], q[b, use[b]:] = math.nan, math.inf, math.nan
+    out, lse = fgmp.tree_attention(q, k, v, made.cache, tree=words, counts=None if counts is None else _i32(counts))
+    _compare_attention(out, lse, q, made, k, v, sees, use, D ** -0.5, H // G)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("H,G,D", [(4, 2, 64), (1, 1, 64), (3, 1, 128), (10, 2, 128), (12, 1, 64), (4, 2, 256)])
@@ -486,6 +509,26 @@ def test_attention_weights_against_their_formula(dtype, D, H, G, T, lens, page, 
     fgmp.attention_weights(q, lse, made.cache, again, rows=_i32(rows), counts=None if counts is None else _i32(counts), max_length=1)
     for b, n in enumerate(lens):
         assert torch.equal(again[b, :, :n], out[b, :, :n]) and bool(torch.isnan(again[b, :, n:]).all())
+
+
+@pytest.mark.parametrize("dtype,D,T,lens,counts", [(BF16, 128, 1024, [1024], None), (BF16, 64, 700, [900, 700], [700, 333]), (F32, 64, 1000, [1300], [999])])
+def test_weights_of_a_chunk_of_a_prompt(dtype, D, T, lens, counts):
+    """As many accepted tokens as a call takes."""
+    _say("weights of a chunk", dtype, D, T, lens, counts)
+    g = _gen(T + D)
+    B, H, G = len(lens), 2, 1
+    made = Made(g, lens, G, D, 64, dtype)
+    q = _randn(g, B, T, H, D, dtype=dtype)
+    use = [T] * B if counts is None else counts
+    lse = torch.full((B, T, H), math.nan, device=DEV)
+    for b, n in enumerate(lens):
+        s = torch.matmul(q[b, : use[b]].double().transpose(0, 1).contiguous(), made.keys[b][:, 0].double().t().contiguous()) * D ** -0.5
+        ends = n - use[b] + torch.arange(use[b], device=DEV) + 1
+        s = s.masked_fill(torch.arange(n, device=DEV) >= ends[:, None], -math.inf)
+        lse[b, : use[b]] = torch.logsumexp(s, -1).t().float()
+    have = torch.rand(B, G, made.slots, generator=g).to(DEV)
+    got = fgmp.attention_weights(q, lse, made.cache, have, counts=None if counts is None else _i32(counts), out=torch.empty_like(have))
+    _compare_weights(got, have, made, q, lse, [list(range(T))] * B, use, D ** -0.5, H // G)
 
 
 def test_weights_of_a_whole_prompt_without_rows():
