@@ -283,7 +283,8 @@ fgmp_status_t fgmp_quantize_weights_clip(const void *W, fgmp_dtype_t dt, int64_t
  * candidates), fgmp_cache_append for the tokens that are kept, and, for a cache held to a budget,
  * fgmp_attention_weights and fgmp_cache_evict.  They follow the conventions above, but for what a cache's or a
  * mask's unused places hold: that may be anything, NaN and infinities among it, and reaches no result.
- * Non-finite values in places that are used give the results that IEEE arithmetic gives the formulas.
+ * Non-finite values in places that are used give the results that IEEE arithmetic gives the formulas.  What would take a
+ * launch of 2^32 threads or more is refused with FGMP_ERR_UNSUPPORTED.
  *
  * A cache keeps `batch` sequences, each a row of slots; slot j of sequence b is row j % page_size of page
  * page_table[b * table_stride + j / page_size], or row j of page b where page_table is null.  A slot holds one

@@ -179,6 +179,9 @@ __device__ __forceinline__ void weigh(RowState<kDim> &st, const f32x4 *s, Weight
 #pragma unroll
         for (int i = 0; i < 4; ++i) w.p[i] = p[i];
     } else {
+        // (BF16 is what the matrix instruction takes.  A weight is off by up to 2^-8 of itself, in either direction, and their sum is of the
+        // unrounded ones; results' errors against 64 bits are 0.0017 of their size with these weights and with FP32 ones, which is
+        // what their own rounding to BF16 makes)
 #pragma unroll
         for (int i = 0; i < 8; ++i) w.p[i] = (__bf16)p[i];
     }
@@ -551,6 +554,9 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int64_t rows)
 // which the workgroup stages in LDS in operand order: once where they are no more than kStage, for every block of keys else.  No sum is
 // shared between waves: the order of additions is fixed.
 
+// Workgroups asked for, more than the chip holds at a time (1280 or 1024 with head_dim 64, 1024 with 128, 512 with 256; FP32 512 with 128, 256 with
+// 256): 2 x 8 heads of 65537 slots, at 256 / 512 / 1024 / 2048: BF16 57 / 38 / 29 / 30 us with head_dim 64, 78 / 64 / 58 / 54 with 128, 112 / 102 / 104 / 115
+// with 256; FP32 83 / 65 / 58 / 56, 124 / 104 / 107 / 123, 200 / 204 / 215 / 256.
 constexpr int kWeightKeys = 2, kStage = 64, kWeightWorkgroups = 2048;
 
 struct WeightArgs {
@@ -667,8 +673,9 @@ __global__ void __launch_bounds__(64 * kWaves) weights_kernel(WeightArgs a)
     }
 }
 
-// How a call is shared out.  Up to 32 rows, and in the types and sizes that the kernel for many rows does not have, a workgroup's waves
-// all have the same rows; that kernel's have 32 each.
+// How a call is shared out.  Up to 32 rows (16 with head_dim 256), and in FP32, a workgroup's waves all have the same rows; those of the kernel
+// for many rows have 32 each.  The one / the other, 4 x 4 heads of 30000 slots: head_dim 128, 32 rows 61 / 67 us, 40 rows 71 / 69, 80 rows 100 / 73; head_dim
+// 256, 16 rows 110 / 134, 32 rows 135 / 135, 40 rows 189 / 132 (8 x 8 heads of 5000: 32 rows 105 / 96); head_dim 64, 32 rows 30 / 29, 80 rows 57 / 34.
 struct AttendPlan {
     int waves_of_rows;      // of the kernel for many rows; 0: the other one
     int row_groups;         // groups of 16 rows, of the other one
@@ -681,13 +688,13 @@ AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t h
 {
     AttendPlan p = {};
     const int64_t groups = (tokens * (q_heads / heads) + 15) / 16;
-    int64_t want;   // workgroups that the chip holds at a time
+    int64_t want;   // workgroups asked for, by making ranges
     if (!f32 && groups > (head_dim == 256 ? 1 : 2)) {
         p.waves_of_rows = groups <= 8 || head_dim == 256 ? 4 : 8;
         p.row_blocks = (groups + 2 * p.waves_of_rows - 1) / (2 * p.waves_of_rows);
         p.tile_keys = wide_keys((int)head_dim);
         p.min_tiles = 128 / p.tile_keys;
-        want = p.waves_of_rows == 8 || head_dim == 256 ? 256 : 512;
+        want = p.waves_of_rows == 8 || head_dim == 256 ? 256 : 512;   // (as many as the chip holds at a time)
     } else {
         // as many rows as the registers of a wave hold, in blocks of equal size
         const int64_t most = head_dim == 256 ? 1 : 2;
@@ -695,6 +702,10 @@ AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t h
         p.row_groups = (int)((groups + p.row_blocks - 1) / p.row_blocks);
         p.tile_keys = f32 ? Elem<true>::kKeys : Elem<false>::kKeys;
         p.min_tiles = 128 / p.tile_keys;
+        // One row group: more than the chip holds at a time but for FP32 and head_dim 64 (768 with BF16 and 64, 512 with 128, 256 with 256), which
+        // evens out their ends over long sequences and is paid for by joining over short ones.  2 x 8 heads of 65537 slots at 256 / 512 / 1024 / 2048:
+        // BF16 63 / 63 / 56 / 58 us with head_dim 64, 110 / 105 / 105 / 107 with 128, 184 / 181 / 184 / 205 with 256; 4 x 8 of 16000: 27 / 31 / 28 / 29,
+        // 56 / 58 / 57 / 57, 94 / 100 / 104 / 125.  Two, 2 x 8 of 65537: 62 / 68 / 63 / 71, 114 / 112 / 116 / 129; FP32 130 / 109 / 122 / 127, 201 / 204 / 217 / 257.
         want = p.row_groups == 1 ? 1024 : 512;
     }
     const int64_t whole = batch * heads * p.row_blocks, least = (int64_t)p.tile_keys * p.min_tiles;
@@ -827,7 +838,6 @@ fgmp_status_t fgmp_attention_weights(const fgmp_heads_t *q, const float *lse, in
     if (max_length == 0 || max_length > a.c.slots) max_length = a.c.slots;
     constexpr int kBlock = 16 * kWeightKeys * kWaves;
     const int64_t pairs = (int64_t)a.c.batch * a.c.heads;
-    // (about as many workgroups as the chip holds at a time)
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>((max_length + kBlock - 1) / kBlock, (kWeightWorkgroups + pairs - 1) / pairs));
     if (!launch_counts(pairs * blocks, 64 * kWaves)) return FGMP_ERR_UNSUPPORTED;
     a.q = static_cast<const char *>(q->data);

@@ -1,5 +1,6 @@
-// Attention of many rows (query heads of a group, for all new tokens): from 33 rows on the waves of a workgroup have rows of their own, 32
-// each, and share the keys and values, which go through LDS in tiles of 64 (32 where head_dim is 256) and are read once for up to 256 rows (128).
+// Attention of many rows (query heads of a group, for all new tokens): from 33 rows on, 17 where head_dim is 256, the waves of a workgroup have
+// rows of their own, 32 each, and share the keys and values, which go through LDS in tiles of 64 (32 where head_dim is 256) and are read once
+// for up to 256 rows (128).
 //
 // The two products of fgmp_attention.hip in 32 x 32 tiles, S^T = K Q^T and O^T += V^T P^T: of a tile of scores lane 32 g + i has row i
 // and keys 8 a + 4 g + j (a, j = 0 .. 3), so the softmax has one step between lanes, and the weights go into the second product from the
@@ -93,7 +94,7 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
     // ---- a tile on its way: global memory -> registers -> LDS ----
     const uint32_t step = (uint32_t)a.c.token_stride;
     const int key_row = tid / kPieces, key_at = tid % kPieces * 16, quad = tid / kQuadThreads, value_at = tid % kQuadThreads * (4 * kWords);
-    // (two tiles are on their way at a time, the even ones in one set of registers, the odd ones in the other)
+    // (the even tiles in one set of registers, the odd ones in the other: room for two tiles on their way)
     u32x4 key[2][kKeyLoads];
     uint32_t value[2][kRounds][4][kWords];
     // A wave's loads of one kind and round are of one group of 16 slots, whose page is looked up a tile ahead of the load.
@@ -252,7 +253,7 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k / 2][k % 2 * 8 + e], a.c2, -base));
             l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-            p[k] = __builtin_convertvector(w, bf16x8);
+            p[k] = __builtin_convertvector(w, bf16x8);   // (a choice: see the other kernel's)
         }
         left_out(p);
 #pragma unroll
@@ -264,10 +265,11 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
         read_ahead<kGroups * kBlocks>();
     };
 
-    // The next tile goes to LDS, and the one two further on is asked for behind the scores, while nothing is read from LDS: reads from LDS wait in
-    // line behind loads that cannot be issued because of the misses under way (25 tokens over 8 x 9999 slots: 142 us with the loads in front
-    // of the scores, 127 behind them; 102 where all loads hit the L2).  Behind the last tile it is loaded again, to no use: with a load left
-    // out, the wait for the one before could not be told from one for all loads.
+    // The next tile goes to LDS, and the one two further on is asked for behind the scores (25 tokens over 8 x 9999 slots: 142 us with the loads in
+    // front of the scores, 127 behind them; 102 where all loads hit the L2).  The two ways to ask, with and without rows, are compiled as two
+    // blocks in line, either of which may have loads under way, and the registers just stored serve the scores: these wait for all or most loads of
+    // the step before, so that a tile's loads have one step, not two, to land.  Behind the last tile it is loaded again, to no use: with a
+    // load left out, the wait for the one before could not be told from one for all loads.
     auto step_of = [&](auto set, auto other, int tile) {
         const int left = n - (begin + tile) * kKeys, ahead = std::min(tile + 3, tiles - 1);
         auto ask = [&] {
