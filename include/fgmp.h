@@ -56,7 +56,8 @@ enum {
     FGMP_ERR_HIP = -6               /* a HIP runtime call failed */
 };
 
-typedef enum { FGMP_F32 = 0, FGMP_BF16 = 1 } fgmp_dtype_t;
+/* FGMP_E4M3 is the dtype of a cache in 8 bits (fgmp_quant_cache_t) and of nothing else. */
+typedef enum { FGMP_F32 = 0, FGMP_BF16 = 1, FGMP_E4M3 = 2 } fgmp_dtype_t;
 
 /* What a block's score measures (the *_ex entry points; the plain ones use FGMP_SCORE_NVFP4_ERROR).
  *   FGMP_SCORE_NVFP4_ERROR  sum_i F_i (x_i - Q_NVFP4(x_i))^2              (Eq. 6)
@@ -402,6 +403,43 @@ fgmp_status_t fgmp_cache_evict(const fgmp_cache_t *cache, const float *weights, 
                                int32_t *positions_out, int32_t *lengths_out, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * ---- A cache in 8 bits ----
+ *
+ * Keys and values as E4M3 codes, with one power of two 2^e for each slot and head, for keys and values apart: an element is code * 2^e.
+ * fgmp_quant_cache_append takes the smallest e from -100 on with which all finite elements of the vector are at most 448 * 2^e in magnitude, and the
+ * nearest codes, ties to even; what is not finite becomes NaN.  Values are exact in FP32 and in BF16 (an element that rounds up to 2^128 becomes infinite).
+ *   codes      a cache as above of dtype FGMP_E4M3: elements of one byte, page_size a multiple of 16 with or without a page table
+ *   k_scales, v_scales   one byte e + 127 for each: of row r of page p and head h at p * scale_page_stride + h * scale_head_stride + r.
+ *              Pointers and strides are multiples of 16 bytes
+ * fgmp_attention_weights and fgmp_cache_evict take no such cache.
+ */
+typedef struct {
+    fgmp_cache_t codes;
+    uint8_t *k_scales, *v_scales;
+    int64_t scale_page_stride, scale_head_stride;
+} fgmp_quant_cache_t;
+
+/* fgmp_tree_attention over a cache in 8 bits: q, k, v and out are BF16, everything else is as there (the workspace, too), and results
+ * are those over a BF16 cache that holds the values fgmp_quant_cache_read gives, but for the order of sums. */
+fgmp_status_t fgmp_quant_cache_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, const fgmp_heads_t *v, int64_t tokens,
+                                         int64_t q_heads, const fgmp_quant_cache_t *cache, const uint64_t *tree, const int32_t *counts,
+                                         float scale, int64_t max_length, const fgmp_heads_t *out, float *lse, void *workspace,
+                                         size_t workspace_bytes, void *stream);
+
+/* fgmp_cache_append into a cache in 8 bits, quantized as it is written; k and v of type `dt`, everything else as there. */
+fgmp_status_t fgmp_quant_cache_append(const fgmp_heads_t *k, const fgmp_heads_t *v, fgmp_dtype_t dt, int64_t tokens,
+                                      const fgmp_quant_cache_t *cache, const int32_t *rows, int64_t accepted, const int32_t *counts,
+                                      int32_t *lengths_out, void *stream);
+
+/*
+ * Slots first .. first + tokens - 1 of every sequence as values, slot first + i of sequence b as token i.
+ *   k_out, v_out   batch x tokens x heads vectors of type `dt`; those of slots that are not in use are left as they are
+ * first + tokens may not exceed the slots that a sequence has.
+ */
+fgmp_status_t fgmp_quant_cache_read(const fgmp_quant_cache_t *cache, int64_t first, int64_t tokens, const fgmp_heads_t *k_out,
+                                    const fgmp_heads_t *v_out, fgmp_dtype_t dt, void *stream);
+
+/*
  * The norms around a block, with its gate and residual scale:
  *   y = residual_scale * x + branch_scale * act(gate) * N(o; post_weight, post_bias)
  *   h = N(y; pre_weight, pre_bias)            with y before it is rounded to its dtype
@@ -423,6 +461,59 @@ fgmp_status_t fgmp_block_norm(const void *x, fgmp_dtype_t x_dt, int64_t ldx, con
                               const float *post_weight, const float *post_bias, const float *pre_weight, const float *pre_bias,
                               fgmp_norm_t kind, float eps, float residual_scale, float branch_scale, void *y, int64_t ldy, void *h,
                               fgmp_dtype_t h_dt, int64_t ldh, void *stream);
+
+/*
+ * Queries, keys and values, as a product leaves them, made ready for attention: queries and keys normed for each head and rotated by
+ * their positions, values converted to the output's type.
+ *   u = w * (x - mean) / sqrt(mean((x - mean)^2) + eps);  FGMP_NORM_RMS: without the mean;  u = x where `w` is null
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = position * inv_freq[i],  of pair i of the first rotary_dim elements of u
+ *   q, k, v    batch x tokens x q_heads, heads, heads vectors of head_dim elements of type `dt`; v, or k and v, nullable, with their outputs
+ *   q_out, ... the same of type `out_dt`; each may be its input itself where the types are alike (the same strides)
+ *   q_weight, k_weight   nullable, FP32, head_dim values, 16-byte aligned
+ *   positions  batch x tokens x axes, without padding
+ *   axis_of    rotary_dim / 2 values: which axis turns pair i (an entry outside 0 .. axes - 1: position 0); nullable where axes is 1
+ *   inv_freq   rotary_dim / 2 FP32 values
+ *   interleaved  zero: pair i is elements i and rotary_dim / 2 + i; else elements 2 i and 2 i + 1
+ * head_dim and rotary_dim multiples of 8, rotary_dim <= head_dim <= 512; rotary_dim 0: norms alone (positions and inv_freq may be null).
+ * Angles are of 64 bits until they are reduced to an eighth of a turn; every number else is FP32 up to the one rounding of an output.
+ */
+fgmp_status_t fgmp_rotate_heads(const fgmp_heads_t *q, const fgmp_heads_t *k, const fgmp_heads_t *v, fgmp_dtype_t dt, int64_t batch,
+                                int64_t tokens, int64_t q_heads, int64_t heads, int64_t head_dim, const float *q_weight,
+                                const float *k_weight, fgmp_norm_t kind, float eps, const int32_t *positions, int64_t axes,
+                                const int32_t *axis_of, const float *inv_freq, int64_t rotary_dim, int interleaved,
+                                const fgmp_heads_t *q_out, const fgmp_heads_t *k_out, const fgmp_heads_t *v_out, fgmp_dtype_t out_dt,
+                                void *stream);
+
+/*
+ * Which drafted tokens of a step are kept, by the target's probabilities, and the token that comes behind them.  Token 0 of a sequence is
+ * certain (the one that the last step ended with); tokens 1 .. tokens - 1 are drafted, each behind its parent, and row t of `target`
+ * is the distribution of what follows token t.  The walk starts at token 0; the children of the token r that it has reached are looked at in their order:
+ *   child t with token x is kept, and the walk goes on from it, if  uniforms[t] * q_t(x) < target[r](x)         with `draft`
+ *                                                                   uniforms[t] * c < target[r](x)              without,
+ * c being 1 less the probabilities of r's children that were refused before t (a token that was refused at r already is refused again).
+ * Where no child is kept, the token behind is drawn from w: max(target[r] - q, 0) where a token drawn from q was refused, target[r] without the
+ * tokens refused at r else: the first j with w_0 + .. + w_j > uniforms[0] * sum w.  So kept and new tokens are distributed as the target's.
+ *   target     batch x tokens rows of `vocab` probabilities of type `dt`, strides in elements, rows contiguous, aligned to an element
+ *   draft      nullable: batch x (tokens - 1) rows, row t - 1 the distribution that token t was drawn from (a chain: `parents` must be null).  Null:
+ *              tokens that were not drawn (the likeliest ones, or ones looked up)
+ *   token_ids  batch x tokens; those of token 0 are not read.  A token outside 0 .. vocab - 1 is refused
+ *   parents    nullable (a chain: t - 1); batch x tokens: the parent of each, before it; entry 0 is not read.  A token whose parent is not before it
+ *              is never reached
+ *   counts     nullable (tokens); per sequence, 0 .. tokens: tokens from counts[b] on are not looked at
+ *   uniforms   batch x tokens numbers in 0 <= u < 1, FP32
+ *   rows       batch x tokens: 0 and the kept tokens, in order, then -1: what fgmp_cache_append takes as rows and, with `accepted`, as counts
+ *   accepted   per sequence: how many those are (token 0 is one of them); 0 where counts[b] is
+ *   next       per sequence: the token behind; -1 where counts[b] is 0 or the row has no probability above 0.  Where nothing is left of w (by
+ *              rounding of the inputs), it is drawn from target[r]
+ *   workspace  >= fgmp_verify_drafts_workspace_bytes; its control region is used
+ * NaN and negative probabilities count as 0.  Sums and comparisons are of 64 bits.  tokens <= 1024, vocab <= 2^24, batch <= 16384.
+ */
+size_t fgmp_verify_drafts_workspace_bytes(int64_t batch, int64_t tokens, int64_t vocab);
+fgmp_status_t fgmp_verify_drafts(const void *target, fgmp_dtype_t dt, int64_t target_batch_stride, int64_t target_row_stride,
+                                 const void *draft, int64_t draft_batch_stride, int64_t draft_row_stride, int64_t batch, int64_t tokens,
+                                 int64_t vocab, const int32_t *token_ids, const int32_t *parents, const int32_t *counts,
+                                 const float *uniforms, int32_t *rows, int32_t *accepted, int32_t *next, void *workspace,
+                                 size_t workspace_bytes, void *stream);
 
 /*
  * Expand a packed tensor to layout-independent arrays (for tests and tools):

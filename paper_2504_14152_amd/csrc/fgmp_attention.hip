@@ -39,6 +39,35 @@ struct Operand {
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) x[p] = *reinterpret_cast<const u32x4 *>(row_and_lane + 64 * p);
     }
+    // in the order that keys of 8 bits have: of every 64 elements the g-th 16, in two pieces; the lane's row + 32 g bytes
+    __device__ __forceinline__ void load_by_64(const char *row_and_lane)
+    {
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) x[p] = *reinterpret_cast<const u32x4 *>(row_and_lane + 128 * (p / 2) + 16 * (p % 2));
+    }
+};
+
+// The same of keys in 8 bits: a load is 16 elements, which become two pieces of BF16 (exactly: a code has 4 bits, its scale is a power of two).
+template <int kDim>
+struct KeyCodes {
+    u32x4 x[kDim / 64];
+    uint32_t scale;
+    __device__ __forceinline__ void load(const char *row_and_lane, const uint8_t *row_scale)
+    {
+#pragma unroll
+        for (int p = 0; p < kDim / 64; ++p) x[p] = *reinterpret_cast<const u32x4 *>(row_and_lane + 64 * p);
+        scale = *row_scale;
+    }
+    __device__ __forceinline__ Operand<false, kDim> values() const
+    {
+        Operand<false, kDim> k;
+        const float s = scale_of(scale);
+#pragma unroll
+        for (int p = 0; p < kDim / 32; ++p)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) k.x[p][w] = values_of(x[p / 2][2 * (p % 2) + w / 2], s, w % 2);
+        return k;
+    }
 };
 
 template <bool kF32, int kDim>
@@ -115,6 +144,35 @@ struct Values {
         for (int p = 0; p < 4; ++p)
             t[p] = __builtin_amdgcn_perm(x[2 * p + 1][m / 2], x[2 * p][m / 2], (m & 1) != 0 ? 0x07060302u : 0x05040100u);
         return __builtin_bit_cast(bf16x8, t);
+    }
+};
+
+// The same of values in 8 bits: lane 16 g + i holds elements n i .. n i + n - 1 of keys 4 g .. 4 g + 3 of each 16, whose scales are a word.
+template <int kDim>
+struct ValueCodes {
+    static constexpr int kWords = kDim / 64;
+    uint32_t x[8][kWords], scale[2];
+    __device__ __forceinline__ void load(int key, const char *at)
+    {
+        if constexpr (kWords == 1) {
+            x[key][0] = *reinterpret_cast<const uint32_t *>(at);
+        } else if constexpr (kWords == 2) {
+            const u32x2 t = *reinterpret_cast<const u32x2 *>(at);
+            x[key][0] = t[0], x[key][1] = t[1];
+        } else {
+            const u32x4 t = *reinterpret_cast<const u32x4 *>(at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[key][e] = t[e];
+        }
+    }
+    __device__ __forceinline__ void values(Values<false, kDim> &v) const
+    {
+#pragma unroll
+        for (int key = 0; key < 8; ++key) {
+            const float s = scale_of(scale[key / 4] >> (8 * (key % 4)) & 0xFFu);
+#pragma unroll
+            for (int w = 0; w < 2 * kWords; ++w) v.x[key][w] = values_of(x[key][w / 2], s, w % 2);
+        }
     }
 };
 
@@ -230,9 +288,11 @@ __device__ __forceinline__ void add_non_finite(RowState<kDim> &st, const f32x4 *
 
 // kRows: groups of 16 rows that a workgroup's waves hold, every wave all of them.  A tile of keys and values is asked for while the one
 // before is worked on: the keys as soon as its scores are there, the values as soon as they have changed places.
-template <bool kF32, int kDim, int kRows>
-__global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(AttendArgs a)
+// kEight: a cache in 8 bits, all else BF16; codes become BF16 when their tile is worked on.
+template <bool kF32, int kDim, int kRows, bool kEight = false>
+__global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(ArgsOf<kEight> a)
 {
+    static_assert(!(kF32 && kEight), "new tokens, results and weights are BF16 where the cache is in 8 bits");
     constexpr int kSize = Elem<kF32>::kSize, kKeys = Elem<kF32>::kKeys, kSubs = kKeys / 16, kPer = kDim / 16;
     constexpr int kLaneKeys = Values<kF32, kDim>::kLaneKeys;
     __shared__ float merge_o[kWaves][kRows * kPer * 4 * 64];
@@ -258,27 +318,48 @@ __global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(
 
     Operand<kF32, kDim> kt[kSubs];
     Values<kF32, kDim> vt;
-    const uint32_t dv = i * kPer * kSize;
+    KeyCodes<kDim> kc[kSubs];                            // (kEight)
+    ValueCodes<kDim> vc;
+    const uint32_t dv = i * kPer * (kEight ? 1 : kSize);
+    const uint8_t *k_scale_at[kSubs], *v_scale_at[kSubs];
     const uint32_t step = (uint32_t)a.c.token_stride;    // (16 rows: less than 2^32 bytes)
     const char *k_at[kSubs], *v_at[kSubs];               // of the tile to be loaded next
     auto locate = [&](int tile) {
 #pragma unroll
         for (int sub = 0; sub < kSubs; ++sub) {
             // (the group of slots behind the last one in use may have no page: read as the one in use)
+            if constexpr (kEight) {
+                uint32_t row;
+                const uint32_t entry = a.c.entry_of((uint32_t)std::min(kSubs * tile + sub, (n - 1) / 16), &row), page = a.c.page_of(b, entry);
+                const int64_t at = a.c.offset(page, row, h), scale = a.scale_at(page, row, h);
+                k_at[sub] = a.c.k + at;
+                v_at[sub] = a.c.v + at;
+                k_scale_at[sub] = a.k_scales + scale;
+                v_scale_at[sub] = a.v_scales + scale;
+                continue;
+            }
             const int64_t at = a.c.group_offset(b, (uint32_t)std::min(kSubs * tile + sub, (n - 1) / 16), h);
             k_at[sub] = a.c.k + at;
             v_at[sub] = a.c.v + at;
         }
+    };
+    auto load_key = [&](int sub, int row) {
+        if constexpr (kEight) kc[sub].load(k_at[sub] + ((uint32_t)row * step + 16u * g), k_scale_at[sub] + (uint32_t)row);
+        else kt[sub].load(k_at[sub] + ((uint32_t)row * step + 16u * g));
+    };
+    auto load_value = [&](int sub, int j, int row) {
+        if constexpr (kEight) vc.load(4 * sub + j, v_at[sub] + ((uint32_t)row * step + dv));
+        else vt.load(4 * sub + j, v_at[sub] + ((uint32_t)row * step + dv));
     };
     // rows behind the last slot in use are read as the last one
     auto load_keys = [&](int tile) {
 #pragma unroll
         for (int sub = 0; sub < kSubs; ++sub) {
             if ((tile + 1) * kKeys <= n) {
-                kt[sub].load(k_at[sub] + ((uint32_t)i * step + 16u * g));
+                load_key(sub, i);
             } else {
                 const int last = std::min(15, n - 1 - 16 * std::min(kSubs * tile + sub, (n - 1) / 16));
-                kt[sub].load(k_at[sub] + ((uint32_t)std::min(i, last) * step + 16u * g));
+                load_key(sub, std::min(i, last));
             }
         }
     };
@@ -287,12 +368,14 @@ __global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(
         for (int sub = 0; sub < kSubs; ++sub) {
             if ((tile + 1) * kKeys <= n) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) vt.load(4 * sub + j, v_at[sub] + ((uint32_t)(4 * g + j) * step + dv));
+                for (int j = 0; j < 4; ++j) load_value(sub, j, 4 * g + j);
             } else {
                 const int last = std::min(15, n - 1 - 16 * std::min(kSubs * tile + sub, (n - 1) / 16));
 #pragma unroll
-                for (int j = 0; j < 4; ++j) vt.load(4 * sub + j, v_at[sub] + ((uint32_t)std::min(4 * g + j, last) * step + dv));
+                for (int j = 0; j < 4; ++j) load_value(sub, j, std::min(4 * g + j, last));
             }
+            // (of slots behind the last one the scales may be anything: their values are cleared)
+            if constexpr (kEight) vc.scale[sub] = *reinterpret_cast<const uint32_t *>(v_scale_at[sub] + 4 * g);
         }
     };
 
@@ -310,7 +393,8 @@ __global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(
         const int row = first + 16 * r + i, t = row / a.group;
         token[r] = t < count ? t : -1;                   // (no row: sees nothing)
         const int at = row < rows ? t : 0, head = h * a.group + (row < rows ? row - t * a.group : 0);
-        q[r].load(a.q + b * a.q_batch + at * a.q_token + head * a.q_head + 16 * g);
+        if constexpr (kEight) q[r].load_by_64(a.q + b * a.q_batch + at * a.q_token + head * a.q_head + 32 * g);
+        else q[r].load(a.q + b * a.q_batch + at * a.q_token + head * a.q_head + 16 * g);
         st[r].m = -INFINITY;
         st[r].l = 0.0f;
 #pragma unroll
@@ -321,11 +405,19 @@ __global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(
         const int next = tile + kWaves, left = n - tile * kKeys;
         if (next < end) locate(next);
         f32x4 s[kRows][kSubs];
+        if constexpr (kEight) {
+#pragma unroll
+            for (int sub = 0; sub < kSubs; ++sub) kt[sub] = kc[sub].values();
+        }
 #pragma unroll
         for (int r = 0; r < kRows; ++r)
 #pragma unroll
             for (int sub = 0; sub < kSubs; ++sub) s[r][sub] = scores<kF32, kDim>(kt[sub], q[r]);
         if (next < end) load_keys(next);
+        if constexpr (kEight) {
+            vc.values(vt);
+            if (next < end) load_values(next);
+        }
         if (left < kKeys) {
             // what lies behind the sequence must not meet a weight of zero: it might not be finite
 #pragma unroll
@@ -353,12 +445,12 @@ __global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) st[r].o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(column, w[r].p, st[r].o[m], 0, 0, 0);
             }
-            if (next < end) load_values(next);
+            if (!kEight && next < end) load_values(next);
         } else {
             bf16x8 columns[kPer];
 #pragma unroll
             for (int m = 0; m < kPer; ++m) columns[m] = vt.column(m);
-            if (next < end) load_values(next);
+            if (!kEight && next < end) load_values(next);
 #pragma unroll
             for (int r = 0; r < kRows; ++r) weigh<kF32, kDim>(st[r], s[r], w[r], a.c2);
 #pragma unroll
@@ -370,10 +462,12 @@ __global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(
         const int start = tile * kKeys, last = drafted - 1 - start;
 #pragma unroll
         for (int sub = 0; sub < kSubs; ++sub) {
-            kt[sub].load(a.k + b * a.k_batch + (start + std::min(16 * sub + i, last)) * a.k_token + h * a.k_head + 16 * g);
+            const char *const key = a.k + b * a.k_batch + (start + std::min(16 * sub + i, last)) * a.k_token + h * a.k_head;
+            if constexpr (kEight) kt[sub].load_by_64(key + 32 * g);
+            else kt[sub].load(key + 16 * g);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                vt.load(4 * sub + j, a.v + b * a.v_batch + (start + std::min(16 * sub + 4 * g + j, last)) * a.v_token + h * a.v_head + dv);
+                vt.load(4 * sub + j, a.v + b * a.v_batch + (start + std::min(16 * sub + 4 * g + j, last)) * a.v_token + h * a.v_head + i * kPer * kSize);
         }
 #pragma unroll
         for (int j = 0; j < kLaneKeys; ++j)
@@ -720,14 +814,14 @@ size_t attend_bytes(const AttendPlan &p, int64_t rows, int64_t head_dim)
     return p.splits > 1 ? (size_t)(rows * p.splits * (head_dim + 2) * 4) : 0;
 }
 
-template <bool kF32, int kDim>
-void attend_launch(const AttendArgs &a, const AttendPlan &p, hipStream_t st)
+template <bool kF32, int kDim, bool kEight = false>
+void attend_launch(const ArgsOf<kEight> &a, const AttendPlan &p, hipStream_t st)
 {
     const dim3 grid((unsigned)p.workgroups);
     if (p.waves_of_rows > 0) attend_wide(a, p.waves_of_rows, (uint32_t)p.workgroups, st);
-    else if (p.row_groups == 1) attend_kernel<kF32, kDim, 1><<<grid, 64 * kWaves, 0, st>>>(a);
+    else if (p.row_groups == 1) attend_kernel<kF32, kDim, 1, kEight><<<grid, 64 * kWaves, 0, st>>>(a);
     if constexpr (kDim != 256) {
-        if (p.row_groups == 2) attend_kernel<kF32, kDim, 2><<<grid, 64 * kWaves, 0, st>>>(a);
+        if (p.row_groups == 2) attend_kernel<kF32, kDim, 2, kEight><<<grid, 64 * kWaves, 0, st>>>(a);
     }
     const int64_t rows = (int64_t)a.c.batch * a.tokens * a.q_heads;
     if (p.splits > 16) join_kernel<kF32, kDim, 4><<<dim3((unsigned)rows), 256, 0, st>>>(a, rows);
@@ -740,32 +834,18 @@ void attend_launch(const AttendArgs &a, const AttendPlan &p, hipStream_t st)
 
 using namespace fgmp;
 
-extern "C" {
-
-size_t fgmp_tree_attention_workspace_bytes(int64_t batch, int64_t tokens, int64_t q_heads, int64_t heads, int64_t head_dim, int64_t max_length)
+// What both calls check and do; the cache is in a already.
+template <bool kEight>
+static fgmp_status_t attend(ArgsOf<kEight> &a, fgmp_dtype_t dtype, const fgmp_heads_t *q, const fgmp_heads_t *k, const fgmp_heads_t *v, int64_t tokens,
+                            int64_t q_heads, const uint64_t *tree, const int32_t *counts, float scale, int64_t max_length, const fgmp_heads_t *out,
+                            float *lse, void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (batch <= 0 || tokens <= 0 || tokens > kMaxTokens || heads <= 0 || q_heads <= 0 || q_heads % heads != 0 || batch > 65535 ||
-        q_heads > 65535 || max_length < 0 || max_length > (int64_t)1 << 30 || (head_dim != 64 && head_dim != 128 && head_dim != 256))
-        return 0;
-    // (the cache's type is not known here: whichever needs more)
-    const AttendPlan p = attend_plan(batch, tokens, q_heads, heads, head_dim, false, max_length);
-    const AttendPlan f = attend_plan(batch, tokens, q_heads, heads, head_dim, true, max_length);
-    const int64_t rows = batch * tokens * q_heads;
-    return std::max<size_t>(16, std::max(attend_bytes(p, rows, head_dim), attend_bytes(f, rows, head_dim)));
-}
-
-fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, const fgmp_heads_t *v, int64_t tokens, int64_t q_heads,
-                                  const fgmp_cache_t *cache, const uint64_t *tree, const int32_t *counts, float scale, int64_t max_length,
-                                  const fgmp_heads_t *out, float *lse, void *workspace, size_t workspace_bytes, void *stream)
-{
-    AttendArgs a = {};
-    fgmp_status_t rc = check_cache(cache, &a.c);
-    if (rc != FGMP_OK) return rc;
+    fgmp_status_t rc;
     if (tokens <= 0 || q_heads <= 0 || lse == nullptr || (k == nullptr) != (v == nullptr) || !(scale > 0.0f) || !(scale < INFINITY) || max_length < 0)
         return FGMP_ERR_INVALID_ARG;
     if (q_heads % a.c.heads != 0) return FGMP_ERR_BAD_SHAPE;
     if (tokens > kMaxTokens || q_heads > 65535) return FGMP_ERR_UNSUPPORTED;
-    const int size = dtype_size(cache->dtype), dim = a.c.head_dim;
+    const int size = dtype_size(dtype), dim = a.c.head_dim;
     if ((rc = check_heads(q, a.c.batch, tokens, q_heads, dim, size, false)) != FGMP_OK) return rc;
     if ((rc = check_heads(out, a.c.batch, tokens, q_heads, dim, size, true)) != FGMP_OK) return rc;
     if (k != nullptr) {
@@ -773,7 +853,7 @@ fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, 
         if ((rc = check_heads(v, a.c.batch, tokens, a.c.heads, dim, size, false)) != FGMP_OK) return rc;
     }
     if (max_length == 0 || max_length > a.c.slots) max_length = a.c.slots;
-    const AttendPlan p = attend_plan(a.c.batch, tokens, q_heads, a.c.heads, dim, cache->dtype == FGMP_F32, max_length);
+    const AttendPlan p = attend_plan(a.c.batch, tokens, q_heads, a.c.heads, dim, dtype == FGMP_F32, max_length);
     const int64_t rows = a.c.batch * tokens * q_heads;
     const size_t need = attend_bytes(p, rows, dim);
     if (need > 0) {
@@ -809,7 +889,11 @@ fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, 
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = a.part_o + rows * p.splits * dim;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (cache->dtype == FGMP_F32) {
+    if constexpr (kEight) {
+        if (dim == 64) attend_launch<false, 64, true>(a, p, st);
+        else if (dim == 128) attend_launch<false, 128, true>(a, p, st);
+        else attend_launch<false, 256, true>(a, p, st);
+    } else if (dtype == FGMP_F32) {
         if (dim == 64) attend_launch<true, 64>(a, p, st);
         else if (dim == 128) attend_launch<true, 128>(a, p, st);
         else attend_launch<true, 256>(a, p, st);
@@ -819,6 +903,44 @@ fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, 
         else attend_launch<false, 256>(a, p, st);
     }
     return hipGetLastError() == hipSuccess ? FGMP_OK : FGMP_ERR_HIP;
+}
+
+extern "C" {
+
+size_t fgmp_tree_attention_workspace_bytes(int64_t batch, int64_t tokens, int64_t q_heads, int64_t heads, int64_t head_dim, int64_t max_length)
+{
+    if (batch <= 0 || tokens <= 0 || tokens > kMaxTokens || heads <= 0 || q_heads <= 0 || q_heads % heads != 0 || batch > 65535 ||
+        q_heads > 65535 || max_length < 0 || max_length > (int64_t)1 << 30 || (head_dim != 64 && head_dim != 128 && head_dim != 256))
+        return 0;
+    // (the cache's type is not known here: whichever needs more)
+    const AttendPlan p = attend_plan(batch, tokens, q_heads, heads, head_dim, false, max_length);
+    const AttendPlan f = attend_plan(batch, tokens, q_heads, heads, head_dim, true, max_length);
+    const int64_t rows = batch * tokens * q_heads;
+    return std::max<size_t>(16, std::max(attend_bytes(p, rows, head_dim), attend_bytes(f, rows, head_dim)));
+}
+
+fgmp_status_t fgmp_tree_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, const fgmp_heads_t *v, int64_t tokens, int64_t q_heads,
+                                  const fgmp_cache_t *cache, const uint64_t *tree, const int32_t *counts, float scale, int64_t max_length,
+                                  const fgmp_heads_t *out, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    AttendArgs a = {};
+    const fgmp_status_t rc = check_cache(cache, &a.c);
+    if (rc != FGMP_OK) return rc;
+    return attend<false>(a, cache->dtype, q, k, v, tokens, q_heads, tree, counts, scale, max_length, out, lse, workspace, workspace_bytes, stream);
+}
+
+fgmp_status_t fgmp_quant_cache_attention(const fgmp_heads_t *q, const fgmp_heads_t *k, const fgmp_heads_t *v, int64_t tokens, int64_t q_heads,
+                                         const fgmp_quant_cache_t *cache, const uint64_t *tree, const int32_t *counts, float scale, int64_t max_length,
+                                         const fgmp_heads_t *out, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    QuantAttendArgs a = {};
+    QuantCacheView c;
+    const fgmp_status_t rc = check_quant_cache(cache, &c);
+    if (rc != FGMP_OK) return rc;
+    a.c = c.c;
+    a.k_scales = c.k_scales, a.v_scales = c.v_scales;
+    a.scale_page = c.scale_page, a.scale_head = c.scale_head;
+    return attend<true>(a, FGMP_BF16, q, k, v, tokens, q_heads, tree, counts, scale, max_length, out, lse, workspace, workspace_bytes, stream);
 }
 
 fgmp_status_t fgmp_attention_weights(const fgmp_heads_t *q, const float *lse, int64_t tokens, int64_t q_heads, const fgmp_cache_t *cache,

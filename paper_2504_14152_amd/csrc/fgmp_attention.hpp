@@ -1,8 +1,9 @@
 // What the attention kernels share: their arguments, how a sequence is split, and steps of the softmax.
 #pragma once
 #include <algorithm>
+#include <type_traits>
 
-#include "fgmp_cache.hpp"
+#include "fgmp_quant_cache.hpp"
 
 namespace fgmp {
 
@@ -44,6 +45,18 @@ struct AttendArgs {
     __device__ __forceinline__ int ranges(int32_t n) const { return std::max(1, (tiles(n) + range(n) - 1) / range(n)); }
 };
 
+// Over a cache in 8 bits.
+struct QuantAttendArgs : AttendArgs {
+    const uint8_t *k_scales, *v_scales;
+    int64_t scale_page, scale_head;       // bytes
+    __device__ __forceinline__ int64_t scale_at(uint32_t page, uint32_t row, int h) const
+    {
+        return (int64_t)(page < c.pages ? page : 0u) * scale_page + (int64_t)h * scale_head + row;
+    }
+};
+template <bool kEight>
+using ArgsOf = std::conditional_t<kEight, QuantAttendArgs, AttendArgs>;
+
 // Which part of the work a workgroup has.  Workgroups go round the XCDs: those of the same rest of 8 follow each other on one XCD.  They
 // are the row blocks of one head's range of keys, of which all but the first find its keys and values in that XCD's L2, then other ranges.
 struct AttendPlace {
@@ -62,6 +75,15 @@ struct AttendPlace {
     }
 };
 
+// Codes of a cache in 8 bits: the value of a scale byte; two values, BF16, of the lower or upper half of a word.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+__device__ __forceinline__ uint32_t values_of(uint32_t codes, float scale, int half)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 x = half != 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false);
+    return __builtin_bit_cast(uint32_t, x);
+}
+
 __device__ __forceinline__ float logsumexp(float most, float l, float c2)
 {
     return l == 0.0f ? -INFINITY : (most * c2 + __builtin_amdgcn_logf(l)) * kLn2;
@@ -72,5 +94,6 @@ __device__ __forceinline__ float inverse_sum(float l) { return l > 0.0f ? 1.0f /
 // BF16: 32 rows in each of 4 or 8 waves, 4 with head_dim 256 (fgmp_attention_wide.hip)
 constexpr int wide_keys(int head_dim) { return head_dim == 256 ? 32 : 64; }
 void attend_wide(const AttendArgs &a, int waves, uint32_t workgroups, hipStream_t st);
+void attend_wide(const QuantAttendArgs &a, int waves, uint32_t workgroups, hipStream_t st);
 
 }  // namespace fgmp

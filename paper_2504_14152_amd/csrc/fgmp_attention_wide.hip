@@ -7,8 +7,6 @@
 // registers they were computed in.  V is transposed on its way into LDS, its keys in the order in which a lane holds the weights.  Two
 // buffers: while one tile is worked on, the next one is in registers on its way; one barrier per tile.  Pieces of 16 bytes
 // change places within an LDS row (by XOR), so that neither the rows written nor the columns read meet in a bank.
-#include <type_traits>
-
 #include "fgmp_attention.hpp"
 
 namespace fgmp {
@@ -61,8 +59,9 @@ __device__ __forceinline__ void read_ahead()
     __builtin_amdgcn_sched_group_barrier(kMatrix, kAhead, 0);
 }
 
-template <int kDim, int kWaves>
-__global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_kernel(AttendArgs a)
+// kEight: a cache in 8 bits, whose codes become BF16 on their way from registers to LDS.
+template <int kDim, int kWaves, bool kEight = false>
+__global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_kernel(ArgsOf<kEight> a)
 {
     typedef float f32x8 __attribute__((ext_vector_type(8)));
     constexpr int kKeys = wide_keys(kDim), kHalves = kKeys / 32, kGroups = kKeys / 16;   // (of 16 keys: slots of one page)
@@ -93,10 +92,13 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
 
     // ---- a tile on its way: global memory -> registers -> LDS ----
     const uint32_t step = (uint32_t)a.c.token_stride;
-    const int key_row = tid / kPieces, key_at = tid % kPieces * 16, quad = tid / kQuadThreads, value_at = tid % kQuadThreads * (4 * kWords);
+    constexpr int kSize = kEight ? 1 : 2, kRaw = kEight ? (kWords + 1) / 2 : kWords;   // of a cached element; words that hold a thread's values of a key
+    const int key_row = tid / kPieces, key_at = tid % kPieces * (8 * kSize), quad = tid / kQuadThreads, value_at = tid % kQuadThreads * (2 * kWords * kSize);
     // (the even tiles in one set of registers, the odd ones in the other: room for two tiles on their way)
-    u32x4 key[2][kKeyLoads];
-    uint32_t value[2][kRounds][4][kWords];
+    typedef std::conditional_t<kEight, u32x2, u32x4> Piece;
+    Piece key[2][kKeyLoads];
+    uint32_t value[2][kRounds][4][kRaw];
+    uint32_t key_scale[2][kEight ? kKeyLoads : 1], value_scale[2][kEight ? kRounds : 1];   // (a byte; a byte for each of four keys)
     // A wave's loads of one kind and round are of one group of 16 slots, whose page is looked up a tile ahead of the load.
     uint32_t key_page[kKeyLoads], value_page[kRounds], key_first[kKeyLoads], value_first[kRounds];
     const int key_group = wave * (64 / kPieces), value_group = wave * (64 / kQuadThreads);   // (in rows, and in quads)
@@ -113,9 +115,11 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
     constexpr std::integral_constant<int, 0> even = {};
     constexpr std::integral_constant<int, 1> odd = {};
     auto load_value = [&](auto set, int r, int j, const char *at) {
-        if constexpr (kWords == 1) {
+        if constexpr (kEight && kWords == 1) {
+            value[set][r][j][0] = *reinterpret_cast<const uint16_t *>(at);
+        } else if constexpr (kRaw == 1) {
             value[set][r][j][0] = *reinterpret_cast<const uint32_t *>(at);
-        } else if constexpr (kWords == 2) {
+        } else if constexpr (kRaw == 2) {
             const u32x2 x = *reinterpret_cast<const u32x2 *>(at);
             value[set][r][j][0] = x[0], value[set][r][j][1] = x[1];
         } else {
@@ -132,7 +136,8 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
             const char *base = a.c.k + a.c.offset(key_page[c], key_first[c], h);
             int r = (key_row + c * kKeyRows) % 16;
             if (left < kKeys && (key_group + c * kKeyRows) / 16 >= (left - 1) / 16) r = std::min(r, (n - 1) & 15);
-            key[set][c] = *reinterpret_cast<const u32x4 *>(base + ((uint32_t)r * step + (uint32_t)key_at));
+            key[set][c] = *reinterpret_cast<const Piece *>(base + ((uint32_t)r * step + (uint32_t)key_at));
+            if constexpr (kEight) key_scale[set][c] = a.k_scales[a.scale_at(key_page[c], key_first[c], h) + r];
         }
     };
     auto load_values = [&](auto set, int tile) {
@@ -147,23 +152,16 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
                 if (last) r = std::min(r, (n - 1) & 15);
                 load_value(set, round, j, base + ((uint32_t)r * step + (uint32_t)value_at));
             }
+            // (of slots behind the last one the scales may be anything: their values are cleared)
+            if constexpr (kEight)
+                value_scale[set][round] = *reinterpret_cast<const uint32_t *>(
+                    a.v_scales + a.scale_at(value_page[round], value_first[round], h) + (quad + round * kQuads) % 4 * 4);
         }
     };
-    auto load_new = [&](int start) {
-#pragma unroll
-        for (int c = 0; c < kKeyLoads; ++c)
-            key[0][c] = *reinterpret_cast<const u32x4 *>(a.k + b * a.k_batch + std::min(start + key_row + c * kKeyRows, drafted - 1) * a.k_token + h * a.k_head + key_at);
-#pragma unroll
-        for (int r = 0; r < kRounds; ++r)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                load_value(even, r, j, a.v + b * a.v_batch + std::min(start + 4 * (quad + r * kQuads) + j, drafted - 1) * a.v_token + h * a.v_head + value_at);
-    };
     // `left`: keys of the tile that there are; what lies behind them must not meet a weight of zero: it might not be finite
-    auto store = [&](auto set, int left) {
-        Tile<kDim> &to = buffer[set];
+    auto put = [&](Tile<kDim> &to, u32x4 *keys, uint32_t (*values)[4][kWords], int left) {
 #pragma unroll
-        for (int c = 0; c < kKeyLoads; ++c) to.k[Tile<kDim>::key_piece(key_row + c * kKeyRows, tid % kPieces)] = key[set][c];
+        for (int c = 0; c < kKeyLoads; ++c) to.k[Tile<kDim>::key_piece(key_row + c * kKeyRows, tid % kPieces)] = keys[c];
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             const int at = quad + r * kQuads;
@@ -171,15 +169,64 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int w = 0; w < kWords; ++w) value[set][r][j][w] = 4 * at + j < left ? value[set][r][j][w] : 0u;
+                    for (int w = 0; w < kWords; ++w) values[r][j][w] = 4 * at + j < left ? values[r][j][w] : 0u;
             }
 #pragma unroll
             for (int m = 0; m < 2 * kWords; ++m) {
                 const uint32_t select = (m & 1) != 0 ? 0x07060302u : 0x05040100u;
-                *to.value_quad(tid % kQuadThreads * (2 * kWords) + m, at) = u32x2{__builtin_amdgcn_perm(value[set][r][1][m / 2], value[set][r][0][m / 2], select),
-                                                                                  __builtin_amdgcn_perm(value[set][r][3][m / 2], value[set][r][2][m / 2], select)};
+                *to.value_quad(tid % kQuadThreads * (2 * kWords) + m, at) = u32x2{__builtin_amdgcn_perm(values[r][1][m / 2], values[r][0][m / 2], select),
+                                                                                  __builtin_amdgcn_perm(values[r][3][m / 2], values[r][2][m / 2], select)};
             }
         }
+    };
+    auto store = [&](auto set, int left) {
+        if constexpr (kEight) {
+            u32x4 keys[kKeyLoads];
+            uint32_t values[kRounds][4][kWords];
+#pragma unroll
+            for (int c = 0; c < kKeyLoads; ++c) {
+                const float scale = scale_of(key_scale[set][c]);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) keys[c][w] = values_of(key[set][c][w / 2], scale, w % 2);
+            }
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float scale = scale_of(value_scale[set][r] >> (8 * j) & 0xFFu);
+#pragma unroll
+                    for (int w = 0; w < kWords; ++w) values[r][j][w] = values_of(value[set][r][j][w / 2], scale, w % 2);
+                }
+            put(buffer[set], keys, values, left);
+        } else {
+            put(buffer[set], key[set], value[set], left);
+        }
+    };
+    // new tokens, which are BF16 whatever the cache is
+    u32x4 new_key[kKeyLoads];
+    uint32_t new_value[kRounds][4][kWords];
+    auto load_new = [&](int start) {
+#pragma unroll
+        for (int c = 0; c < kKeyLoads; ++c)
+            new_key[c] = *reinterpret_cast<const u32x4 *>(a.k + b * a.k_batch + std::min(start + key_row + c * kKeyRows, drafted - 1) * a.k_token + h * a.k_head +
+                                                          tid % kPieces * 16);
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const char *at = a.v + b * a.v_batch + std::min(start + 4 * (quad + r * kQuads) + j, drafted - 1) * a.v_token + h * a.v_head +
+                                 tid % kQuadThreads * (4 * kWords);
+                if constexpr (kWords == 1) {
+                    new_value[r][j][0] = *reinterpret_cast<const uint32_t *>(at);
+                } else if constexpr (kWords == 2) {
+                    const u32x2 x = *reinterpret_cast<const u32x2 *>(at);
+                    new_value[r][j][0] = x[0], new_value[r][j][1] = x[1];
+                } else {
+                    const u32x4 x = *reinterpret_cast<const u32x4 *>(at);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) new_value[r][j][w] = x[w];
+                }
+            }
     };
 
     u32x4 q[kSteps];      // lane 32 g + i: row i, of every 32 bytes the g-th 16
@@ -310,11 +357,11 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int w = 0; w < kWords; ++w) {
-                    fine = fine && (finite_pair(value[0][r][j][w]) || 4 * (quad + r * kQuads) + j >= here);
-                    value[0][r][j][w] = finite_part(value[0][r][j][w]);
+                    fine = fine && (finite_pair(new_value[r][j][w]) || 4 * (quad + r * kQuads) + j >= here);
+                    new_value[r][j][w] = finite_part(new_value[r][j][w]);
                 }
         if (!fine) not_finite = start;
-        store(even, here);
+        put(buffer[0], new_key, new_value, here);
         __syncthreads();
         uint64_t sees = 0ull;
         if (t < count) {
@@ -383,22 +430,27 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
     }
 }
 
-template <int kDim>
-void launch(const AttendArgs &a, int waves, const dim3 grid, hipStream_t st)
+template <int kDim, bool kEight>
+void launch(const ArgsOf<kEight> &a, int waves, const dim3 grid, hipStream_t st)
 {
-    if (waves == 4) attend_wide_kernel<kDim, 4><<<grid, 256, 0, st>>>(a);
+    if (waves == 4) attend_wide_kernel<kDim, 4, kEight><<<grid, 256, 0, st>>>(a);
     if constexpr (kDim != 256) {
-        if (waves == 8) attend_wide_kernel<kDim, 8><<<grid, 512, 0, st>>>(a);
+        if (waves == 8) attend_wide_kernel<kDim, 8, kEight><<<grid, 512, 0, st>>>(a);
     }
+}
+
+template <bool kEight>
+void launch(const ArgsOf<kEight> &a, int waves, uint32_t workgroups, hipStream_t st)
+{
+    const dim3 grid(workgroups);
+    if (a.c.head_dim == 64) launch<64, kEight>(a, waves, grid, st);
+    else if (a.c.head_dim == 128) launch<128, kEight>(a, waves, grid, st);
+    else launch<256, kEight>(a, waves, grid, st);
 }
 
 }  // namespace
 
-void attend_wide(const AttendArgs &a, int waves, uint32_t workgroups, hipStream_t st)
-{
-    if (a.c.head_dim == 64) launch<64>(a, waves, dim3(workgroups), st);
-    else if (a.c.head_dim == 128) launch<128>(a, waves, dim3(workgroups), st);
-    else launch<256>(a, waves, dim3(workgroups), st);
-}
+void attend_wide(const AttendArgs &a, int waves, uint32_t workgroups, hipStream_t st) { launch<false>(a, waves, workgroups, st); }
+void attend_wide(const QuantAttendArgs &a, int waves, uint32_t workgroups, hipStream_t st) { launch<true>(a, waves, workgroups, st); }
 
 }  // namespace fgmp

@@ -7,11 +7,17 @@ namespace fgmp {
 
 fgmp_status_t check_cache(const fgmp_cache_t *c, CacheView *view)
 {
-    if (c == nullptr || c->k == nullptr || c->v == nullptr || c->lengths == nullptr || !known_dtype(c->dtype)) return FGMP_ERR_INVALID_ARG;
+    if (c == nullptr || !known_dtype(c->dtype)) return FGMP_ERR_INVALID_ARG;
+    return check_cache_of(c, dtype_size(c->dtype), view);
+}
+
+fgmp_status_t check_cache_of(const fgmp_cache_t *c, int size, CacheView *view)
+{
+    if (c->k == nullptr || c->v == nullptr || c->lengths == nullptr) return FGMP_ERR_INVALID_ARG;
     if (c->batch <= 0 || c->heads <= 0 || c->page_size <= 0 || c->pages_per_sequence <= 0 || c->pages <= 0) return FGMP_ERR_INVALID_ARG;
     if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return FGMP_ERR_UNSUPPORTED;
     const bool paged = c->page_table != nullptr;
-    const int size = dtype_size(c->dtype), unit = 16 / size;
+    const int unit = 16 / size;
     if (paged ? c->page_size % kSlotGroup != 0 || c->table_stride < c->pages_per_sequence : c->pages_per_sequence != 1 || c->pages < c->batch)
         return FGMP_ERR_BAD_SHAPE;
     // (the stride of a single page or head is taken times zero)

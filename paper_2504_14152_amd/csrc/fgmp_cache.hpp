@@ -61,6 +61,7 @@ inline bool known_dtype(fgmp_dtype_t dt) { return dt == FGMP_F32 || dt == FGMP_B
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0u; }
 
 fgmp_status_t check_cache(const fgmp_cache_t *c, CacheView *view);
+fgmp_status_t check_cache_of(const fgmp_cache_t *c, int size, CacheView *view);   // elements of `size` bytes, whatever the dtype says
 // batch x tokens x heads vectors of `dim` elements of `size` bytes; `written`: no two of them may share memory
 fgmp_status_t check_heads(const fgmp_heads_t *x, int64_t batch, int64_t tokens, int64_t heads, int dim, int size, bool written);
 

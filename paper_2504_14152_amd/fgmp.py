@@ -15,7 +15,7 @@ import torch
 
 from . import build as _build
 
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 _ERRORS = {-1: "INVALID_ARG", -2: "BAD_SHAPE", -3: "BAD_ALIGN", -4: "BUFFER_TOO_SMALL",
            -5: "UNSUPPORTED", -6: "HIP_ERROR"}
 _lib = None
@@ -32,6 +32,11 @@ class _CacheStruct(ctypes.Structure):
                 ("pages_per_sequence", ctypes.c_int32), ("pages", ctypes.c_int64), ("page_stride", ctypes.c_int64),
                 ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("page_table", ctypes.c_void_p),
                 ("table_stride", ctypes.c_int64), ("lengths", ctypes.c_void_p)]
+
+
+class _QuantCacheStruct(ctypes.Structure):
+    _fields_ = [("codes", _CacheStruct), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("scale_page_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64)]
 
 
 class _HeadsStruct(ctypes.Structure):
@@ -156,7 +161,8 @@ def _load(path: str) -> ctypes.CDLL:
                                         vp, sz, vp]
     L.fused_entry = ctypes.cast(L.fgmp_quant_gemm_fused, ctypes.c_void_p).value
     L.entries = {n: ctypes.cast(getattr(L, "fgmp_" + n), ctypes.c_void_p).value
-                 for n in ("tree_attention", "attention_weights", "cache_append", "cache_evict", "block_norm")}
+                 for n in ("tree_attention", "attention_weights", "cache_append", "cache_evict", "block_norm", "quant_cache_attention",
+                           "quant_cache_append", "quant_cache_read", "rotate_heads", "verify_drafts")}
     L.fgmp_quant_gemm_fused_static_scratch.restype = ctypes.c_int
     L.fgmp_quant_gemm_fused_static_scratch.argtypes = [vp, ctypes.c_int, i64, i64, i64, vp, f32, f32, vp, i64, vp, i64, vp]
     L.fgmp_unpack_canonical.restype = ctypes.c_int
@@ -185,6 +191,19 @@ def _load(path: str) -> ctypes.CDLL:
     L.fgmp_cache_evict_workspace_bytes.argtypes = [i64, i64, i64, i64]
     L.fgmp_cache_evict.restype = ctypes.c_int
     L.fgmp_cache_evict.argtypes = [cache, vp, vp, i64, vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]
+    quant, i32 = ctypes.POINTER(_QuantCacheStruct), ctypes.c_int
+    L.fgmp_quant_cache_attention.restype = i32
+    L.fgmp_quant_cache_attention.argtypes = [heads, heads, heads, i64, i64, quant, vp, vp, f32, i64, heads, vp, vp, sz, vp]
+    L.fgmp_quant_cache_append.restype = i32
+    L.fgmp_quant_cache_append.argtypes = [heads, heads, i32, i64, quant, vp, i64, vp, vp, vp]
+    L.fgmp_quant_cache_read.restype = i32
+    L.fgmp_quant_cache_read.argtypes = [quant, i64, i64, heads, heads, i32, vp]
+    L.fgmp_rotate_heads.restype = i32
+    L.fgmp_rotate_heads.argtypes = [heads, heads, heads, i32, i64, i64, i64, i64, i64, vp, vp, i32, f32, vp, i64, vp, vp, i64, i32, heads, heads, heads, i32, vp]
+    L.fgmp_verify_drafts_workspace_bytes.restype = sz
+    L.fgmp_verify_drafts_workspace_bytes.argtypes = [i64, i64, i64]
+    L.fgmp_verify_drafts.restype = i32
+    L.fgmp_verify_drafts.argtypes = [vp, i32, i64, i64, vp, i64, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.fgmp_block_norm.restype = ctypes.c_int
     L.fgmp_block_norm.argtypes = [vp, ctypes.c_int, i64, vp, ctypes.c_int, i64, vp, i64, i64, ctypes.c_int, i64, i64, vp, vp, vp, vp,
                                   ctypes.c_int, f32, f32, f32, vp, i64, vp, ctypes.c_int, i64, vp]
@@ -564,12 +583,16 @@ def selftest_decode_table(fmt: int, device="cuda"):
 _TYPES = (torch.float32, torch.bfloat16, torch.int32, torch.int64, torch.uint8)
 
 
+def _not_handed(*args) -> None:
+    return None
+
+
 def _handed(name: str, *args) -> bool:
     """Whether the extension module took a call's arguments as they are (and the call went well); otherwise nothing has happened, and the
     general path has something to make, to refuse or to say."""
     if _call is None:
         return False
-    rc = getattr(_call, name)(lib().entries[name], _TYPES, *args, _stream())
+    rc = getattr(_call, name, _not_handed)(lib().entries[name], _TYPES, *args, _stream())
     if rc is None:
         return False
     if rc != 0:
@@ -615,6 +638,48 @@ class Cache:
         self._struct.lengths = value.data_ptr()
 
 
+class QuantCache:
+    """The same in 8 bits (fgmp_quant_cache_t): `k` and `v` pages x page_size x heads x head_dim codes (float8_e4m3fn), `k_scales` and `v_scales`
+    pages x heads x page_size scale bytes (uint8, of the same strides, the last dimension contiguous); page_size a multiple of 16, with or without a
+    `page_table`.  tree_attention and cache_append take either kind of cache, cache_read this one.  A new one's codes and scales may hold
+    anything: only slots in use are read."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor, lengths: torch.Tensor,
+                 page_table: torch.Tensor | None = None):
+        _require_cuda(k, v, k_scales, v_scales, lengths, page_table)
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != torch.float8_e4m3fn or v.dtype != k.dtype or k.stride(3) != 1:
+            raise FgmpError("k and v: the same pages x page_size x heads x head_dim of float8_e4m3fn, head_dim contiguous")
+        pages, page_size, heads, dim = k.shape
+        for s in (k_scales, v_scales):
+            if s.dtype != torch.uint8 or s.shape != (pages, heads, page_size) or s.stride() != k_scales.stride() or s.stride(2) != 1:
+                raise FgmpError("k_scales and v_scales: the same pages x heads x page_size of uint8, page_size contiguous")
+        if page_table is not None:
+            _check_int32(page_table, "page_table")
+            if page_table.dim() != 2 or page_table.stride(1) != 1 or page_table.shape[0] != lengths.shape[0]:
+                raise FgmpError("page_table: batch x pages per sequence, rows contiguous")
+        self.k, self.v, self.k_scales, self.v_scales, self.page_table = k, v, k_scales, v_scales, page_table
+        self.batch, self.heads, self.head_dim, self.dtype = lengths.shape[0], heads, dim, torch.bfloat16
+        per = 1 if page_table is None else page_table.shape[1]
+        self.slots = per * page_size
+        codes = _CacheStruct(k.data_ptr(), v.data_ptr(), E4M3, self.batch, heads, dim, page_size, per, pages, k.stride(0), k.stride(1), k.stride(2),
+                             _ptr(page_table), 0 if page_table is None else page_table.stride(0), None)
+        self._struct = _QuantCacheStruct(codes, k_scales.data_ptr(), v_scales.data_ptr(), k_scales.stride(0), k_scales.stride(1))
+        self._ref = ctypes.byref(self._struct)
+        self._handle = (ctypes.addressof(self._struct), self.batch, heads, dim, self.slots, torch.bfloat16)
+        self.lengths = lengths
+
+    @property
+    def lengths(self) -> torch.Tensor:
+        return self._lengths
+
+    @lengths.setter
+    def lengths(self, value: torch.Tensor) -> None:
+        _require_cuda(value)
+        _check_int32(value, "lengths", (self.batch,))
+        self._lengths = value
+        self._struct.codes.lengths = value.data_ptr()
+
+
 def _check_int32(t: torch.Tensor | None, what: str, shape: tuple | None = None) -> None:
     """int32 and, where a shape is asked for, contiguous of that shape."""
     if t is not None and (t.dtype != torch.int32 or (shape is not None and (t.shape != shape or not t.is_contiguous()))):
@@ -654,14 +719,16 @@ def tree_attention_workspace_bytes(batch: int, tokens: int, q_heads: int, heads:
     return int(lib().fgmp_tree_attention_workspace_bytes(batch, tokens, q_heads, heads, head_dim, max_length))
 
 
-def tree_attention(q: torch.Tensor, k: torch.Tensor | None, v: torch.Tensor | None, cache: Cache, tree: torch.Tensor | None = None,
+def tree_attention(q: torch.Tensor, k: torch.Tensor | None, v: torch.Tensor | None, cache: Cache | QuantCache, tree: torch.Tensor | None = None,
                    counts: torch.Tensor | None = None, scale: float | None = None, max_length: int = 0, out: torch.Tensor | None = None,
                    lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """(out, lse) of new tokens' attention over a cache and each other: q batch x tokens x query heads x head_dim; k, v batch x tokens x
     heads x head_dim, or None.  `tree`: batch x tokens x words (int64, see tree_words), None for a chain; `counts` (int32): new tokens
-    of each sequence; `scale` 1 / sqrt(head_dim) unless given; `max_length`: the longest sequence, where the caller knows it."""
+    of each sequence; `scale` 1 / sqrt(head_dim) unless given; `max_length`: the longest sequence, where the caller knows it.  q, k, v and out
+    are of the cache's type, BF16 over a QuantCache."""
+    entry = "quant_cache_attention" if type(cache) is QuantCache else "tree_attention"
     if out is not None and lse is not None and workspace is not None and scale is not None and _handed(
-            "tree_attention", q, k, v, cache._handle, tree, counts, scale, max_length, out, lse, workspace):
+            entry, q, k, v, cache._handle, tree, counts, scale, max_length, out, lse, workspace):
         return out, lse
     _require_cuda(q, k, v, tree, counts, out, lse, workspace)
     if q.dim() != 4 or (k is None) != (v is None):
@@ -681,11 +748,11 @@ def tree_attention(q: torch.Tensor, k: torch.Tensor | None, v: torch.Tensor | No
     if workspace is None:
         workspace = torch.empty(tree_attention_workspace_bytes(B, T, H, cache.heads, D, max_length or cache.slots), dtype=torch.uint8,
                                 device=q.device)
-    rc = lib().fgmp_tree_attention(_heads(q, "q", (B, T, H, D), dtype), None if k is None else _heads(k, "k", new, dtype),
-                                   None if v is None else _heads(v, "v", new, dtype), T, H, cache._ref, _ptr(tree), _ptr(counts),
-                                   D ** -0.5 if scale is None else scale, max_length, _heads(out, "out", (B, T, H, D), dtype),
-                                   lse.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream())
-    _check(rc, "fgmp_tree_attention")
+    rc = getattr(lib(), "fgmp_" + entry)(_heads(q, "q", (B, T, H, D), dtype), None if k is None else _heads(k, "k", new, dtype),
+                                         None if v is None else _heads(v, "v", new, dtype), T, H, cache._ref, _ptr(tree), _ptr(counts),
+                                         D ** -0.5 if scale is None else scale, max_length, _heads(out, "out", (B, T, H, D), dtype),
+                                         lse.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream())
+    _check(rc, "fgmp_" + entry)
     return out, lse
 
 
@@ -694,6 +761,7 @@ def attention_weights(q: torch.Tensor, lse: torch.Tensor, cache: Cache, weights:
     """`weights` (batch x heads x slots, float32) and what the accepted tokens' attention adds to it, in `out` (`weights` itself unless
     given): call it after cache_append, with the q and lse that tree_attention took and gave.  `rows` (int32, batch x accepted): which
     rows of q were accepted; `counts` (int32): how many of them, and were stored: the growth of the lengths, where the cache may be full."""
+    _require_plain(cache, "attention_weights")
     if scale is not None and _handed("attention_weights", q, lse, cache._handle, weights, rows, counts, scale, max_length,
                                      weights if out is None else out):
         return weights if out is None else out
@@ -714,6 +782,11 @@ def attention_weights(q: torch.Tensor, lse: torch.Tensor, cache: Cache, weights:
     return out
 
 
+def _require_plain(cache, what: str) -> None:
+    if type(cache) is QuantCache:
+        raise FgmpError(f"{what} takes no QuantCache")
+
+
 def _accepted(rows: torch.Tensor | None, counts: torch.Tensor | None, B: int, T: int) -> int:
     accepted = T if rows is None else rows.shape[-1]
     _check_int32(rows, "rows", (B, accepted))
@@ -721,13 +794,17 @@ def _accepted(rows: torch.Tensor | None, counts: torch.Tensor | None, B: int, T:
     return accepted
 
 
-def cache_append(k: torch.Tensor, v: torch.Tensor, cache: Cache, rows: torch.Tensor | None = None, counts: torch.Tensor | None = None,
+def cache_append(k: torch.Tensor, v: torch.Tensor, cache: Cache | QuantCache, rows: torch.Tensor | None = None, counts: torch.Tensor | None = None,
                  positions: torch.Tensor | None = None, slot_positions: torch.Tensor | None = None,
                  slot_weights: torch.Tensor | None = None, lengths_out: torch.Tensor | None = None) -> torch.Tensor:
     """Keys and values of accepted tokens (`rows`, `counts` as attention_weights; k, v as tree_attention, float32 too) into the next slots
     of the cache; returns the new lengths, for cache.lengths.  `positions` (int32, batch x tokens) go to `slot_positions` (int32, batch x
     heads x slots); `slot_weights` (float32) of new slots become 0.  Tokens without a slot are dropped: the new lengths less the old ones are the
-    `counts` that were stored."""
+    `counts` that were stored.  Into a QuantCache they go quantized (fgmp_quant_cache_append), without `slot_positions` and `slot_weights`."""
+    if type(cache) is QuantCache:
+        if slot_positions is not None or slot_weights is not None:
+            raise FgmpError("a QuantCache has no slot_positions and slot_weights")
+        return _quant_append(k, v, cache, rows, counts, lengths_out)
     if lengths_out is not None and _handed("cache_append", k, v, cache._handle, rows, counts, positions, slot_positions, slot_weights, lengths_out):
         return lengths_out
     _require_cuda(k, v, rows, counts, positions, slot_positions, slot_weights, lengths_out)
@@ -750,6 +827,50 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, cache: Cache, rows: torch.Ten
     return lengths_out
 
 
+def _quant_append(k, v, cache: QuantCache, rows, counts, lengths_out) -> torch.Tensor:
+    if lengths_out is not None and _handed("quant_cache_append", k, v, cache._handle, rows, counts, lengths_out):
+        return lengths_out
+    _require_cuda(k, v, rows, counts, lengths_out)
+    if k.dim() != 4 or k.dtype != v.dtype:
+        raise FgmpError("k and v: batch x tokens x heads x head_dim, of one type")
+    T, shape = k.shape[1], (cache.batch, k.shape[1], cache.heads, cache.head_dim)
+    accepted = _accepted(rows, counts, cache.batch, T)
+    if lengths_out is None:
+        lengths_out = torch.empty(cache.batch, dtype=torch.int32, device=k.device)
+    _check_int32(lengths_out, "lengths_out", (cache.batch,))
+    rc = lib().fgmp_quant_cache_append(_heads(k, "k", shape), _heads(v, "v", shape), _dtype_code(k), T, cache._ref, _ptr(rows), accepted,
+                                       _ptr(counts), lengths_out.data_ptr(), _stream())
+    _check(rc, "fgmp_quant_cache_append")
+    return lengths_out
+
+
+def cache_read(cache: QuantCache, first: int = 0, tokens: int | None = None, k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None,
+               dtype: torch.dtype = torch.bfloat16):
+    """(k, v) of slots first .. first + tokens - 1 of every sequence (fgmp_quant_cache_read), batch x tokens x heads x head_dim: in `k_out` and
+    `v_out`, whose size and type say how many and of what type, or in new ones of `dtype`, zeros where a slot is not in use; `tokens`: up to the last
+    slot unless given.  In outputs that are given, places of slots not in use are left as they are."""
+    if type(cache) is not QuantCache:
+        raise FgmpError("cache_read takes a QuantCache")
+    if k_out is not None and v_out is not None and tokens is None and _handed("quant_cache_read", cache._handle, first, k_out, v_out):
+        return k_out, v_out
+    _require_cuda(k_out, v_out)
+    given = k_out if k_out is not None else v_out
+    if given is not None:
+        if given.dim() != 4 or (tokens is not None and tokens != given.shape[1]):
+            raise FgmpError("k_out and v_out: batch x tokens x heads x head_dim")
+        tokens, dtype = given.shape[1], given.dtype
+    elif tokens is None:
+        tokens = cache.slots - first
+    if tokens <= 0 or first < 0 or first + tokens > cache.slots:
+        raise FgmpError(f"slots {first} to {first + tokens}: a sequence has {cache.slots}")
+    shape = (cache.batch, tokens, cache.heads, cache.head_dim)
+    k_out, v_out = (torch.zeros(shape, dtype=dtype, device=cache.k.device) if t is None else t for t in (k_out, v_out))
+    rc = lib().fgmp_quant_cache_read(cache._ref, first, tokens, _heads(k_out, "k_out", shape, dtype), _heads(v_out, "v_out", shape, dtype),
+                                     _dtype_code(k_out), _stream())
+    _check(rc, "fgmp_quant_cache_read")
+    return k_out, v_out
+
+
 def cache_evict_workspace_bytes(batch: int, heads: int, slots: int, budget: int) -> int:
     return int(lib().fgmp_cache_evict_workspace_bytes(batch, heads, slots, budget))
 
@@ -759,6 +880,7 @@ def cache_evict(cache: Cache, weights: torch.Tensor, positions: torch.Tensor, se
                 lengths_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """Cuts every sequence to `budget` slots by accumulated attention weight (fgmp_cache_evict): keys and values move within the cache;
     returns (weights, positions, lengths), the first two in place unless `weights_out` and `positions_out` are given."""
+    _require_plain(cache, "cache_evict")
     weights_out = weights if weights_out is None else weights_out
     positions_out = positions if positions_out is None else positions_out
     if lengths_out is not None and workspace is not None and _handed(
@@ -823,3 +945,94 @@ def block_norm(x: torch.Tensor, o: torch.Tensor | None = None, post_weight: torc
                                0 if h is None else _dtype_code(h), 0 if h is None else h.stride(0), _stream())
     _check(rc, "fgmp_block_norm")
     return (x if o is None else out), h
+
+
+def rotary_axes(sections) -> torch.Tensor:
+    """The `axes` of rotate_heads (int32, on the CPU) for pairs dealt out in runs: `sections[i]` pairs turn by axis i."""
+    return torch.cat([torch.full((int(n),), i, dtype=torch.int32) for i, n in enumerate(sections)])
+
+
+def rotate_heads(q: torch.Tensor, k: torch.Tensor | None = None, v: torch.Tensor | None = None, positions: torch.Tensor | None = None,
+                 inv_freq: torch.Tensor | None = None, axes: torch.Tensor | None = None, q_weight: torch.Tensor | None = None,
+                 k_weight: torch.Tensor | None = None, kind: str = "rms", eps: float = 1e-5, interleaved: bool = False,
+                 q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None,
+                 dtype: torch.dtype = torch.bfloat16):
+    """(q, k, v) ready for attention (fgmp_rotate_heads): q and k, batch x tokens x heads x head_dim, normed for each head where `q_weight` and
+    `k_weight` (float32) are given and their first 2 len(inv_freq) elements rotated by `positions` (int32, batch x tokens, or batch x tokens x axes with
+    `axes`, which axis each pair turns by, see rotary_axes); v converted.  Without `inv_freq` nothing is rotated.  Outputs are made in `dtype` where they are
+    not given; each may be its input itself.  k and v may be None."""
+    if q_out is not None and (k is None) == (k_out is None) and (v is None) == (v_out is None) and inv_freq is not None and kind in NORMS and _handed(
+            "rotate_heads", q, k, v, positions, inv_freq, axes, q_weight, k_weight, NORMS[kind], eps, interleaved, q_out, k_out, v_out):
+        return q_out, k_out, v_out
+    _require_cuda(q, k, v, positions, inv_freq, axes, q_weight, k_weight, q_out, k_out, v_out)
+    if q.dim() != 4 or (k is None and v is not None) or (k is None and k_out is not None) or (v is None and v_out is not None):
+        raise FgmpError("q: batch x tokens x heads x head_dim; v only with k, outputs only of what is given")
+    if kind not in NORMS:
+        raise FgmpError(f"kind: one of {sorted(NORMS)}")
+    B, T, H, D = q.shape
+    G = 0 if k is None else k.shape[2]
+    pairs = 0 if inv_freq is None else inv_freq.shape[0]
+    n_axes = 1 if positions is None or positions.dim() == 2 else positions.shape[-1]
+    if pairs > 0:
+        _check_f32(inv_freq, "inv_freq", (pairs,))
+        if positions is None or (axes is None and n_axes > 1):
+            raise FgmpError("positions: batch x tokens, or batch x tokens x axes with `axes`")
+        _check_int32(positions, "positions", (B, T) if positions.dim() == 2 else (B, T, n_axes))
+        _check_int32(axes, "axes", (pairs,))
+    _check_f32(q_weight, "q_weight", (D,))
+    _check_f32(k_weight, "k_weight", (D,))
+    given = next((t for t in (q_out, k_out, v_out) if t is not None), None)
+    dtype = dtype if given is None else given.dtype
+    shapes = ((B, T, H, D), (B, T, G, D), (B, T, G, D))
+    outs = [None if t is None else torch.empty(shape, dtype=dtype, device=q.device) if o is None else o
+            for t, o, shape in zip((q, k, v), (q_out, k_out, v_out), shapes)]
+
+    def at(t, name, shape, kind_of):
+        return None if t is None else _heads(t, name, shape, kind_of)
+
+    sources = [at(t, name, shape, q.dtype) for t, name, shape in zip((q, k, v), "qkv", shapes)]
+    targets = [at(t, name + "_out", shape, dtype) for t, name, shape in zip(outs, "qkv", shapes)]
+    rc = lib().fgmp_rotate_heads(*sources, _dtype_code(q), B, T, H, G, D, _ptr(q_weight), _ptr(k_weight), NORMS[kind], eps, _ptr(positions), n_axes,
+                                 _ptr(axes), _ptr(inv_freq), 2 * pairs, int(interleaved), *targets, _dtype_code(outs[0]), _stream())
+    _check(rc, "fgmp_rotate_heads")
+    return tuple(outs)
+
+
+def verify_drafts_workspace_bytes(batch: int, tokens: int, vocab: int) -> int:
+    return int(lib().fgmp_verify_drafts_workspace_bytes(batch, tokens, vocab))
+
+
+def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, uniforms: torch.Tensor, draft: torch.Tensor | None = None,
+                  parents: torch.Tensor | None = None, counts: torch.Tensor | None = None, rows: torch.Tensor | None = None,
+                  accepted: torch.Tensor | None = None, next_tokens: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """(rows, accepted, next_tokens): which drafted tokens the target keeps, and the token behind them (fgmp_verify_drafts).  `target` batch x tokens x
+    vocab probabilities, row t those of what follows token t; `tokens` (int32, batch x tokens) with the certain token first; `uniforms` (float32) like
+    them, the first one for the token behind; `draft` batch x tokens - 1 x vocab, what tokens 1, 2, .. of a chain were drawn from; `parents` (int32) of
+    a tree, as tree_words takes them.  `rows` (-1 behind the last) and `accepted` (token 0 counts) are what cache_append takes as rows and counts."""
+    if rows is not None and accepted is not None and next_tokens is not None and workspace is not None and _handed(
+            "verify_drafts", target, tokens, uniforms, draft, parents, counts, rows, accepted, next_tokens, workspace):
+        return rows, accepted, next_tokens
+    _require_cuda(target, tokens, uniforms, draft, parents, counts, rows, accepted, next_tokens, workspace)
+    if target.dim() != 3 or target.stride(2) != 1:
+        raise FgmpError("target: batch x tokens x vocab, rows contiguous")
+    B, N, V = target.shape
+    if draft is not None:
+        if parents is not None:
+            raise FgmpError("draft goes with a chain, not with parents")
+        if draft.dtype != target.dtype or draft.shape != (B, N - 1, V) or draft.stride(2) != 1:
+            raise FgmpError("draft: batch x tokens - 1 x vocab, of target's type, rows contiguous")
+    rows = torch.empty((B, N), dtype=torch.int32, device=target.device) if rows is None else rows
+    accepted, next_tokens = (torch.empty(B, dtype=torch.int32, device=target.device) if t is None else t for t in (accepted, next_tokens))
+    for t, name, shape in ((tokens, "tokens", (B, N)), (parents, "parents", (B, N)), (counts, "counts", (B,)), (rows, "rows", (B, N)),
+                           (accepted, "accepted", (B,)), (next_tokens, "next_tokens", (B,))):
+        _check_int32(t, name, shape)
+    _check_f32(uniforms, "uniforms", (B, N))
+    if workspace is None:
+        workspace = new_workspace(verify_drafts_workspace_bytes(B, N, V), target.device)
+    rc = lib().fgmp_verify_drafts(target.data_ptr(), _dtype_code(target), target.stride(0), target.stride(1),
+                                  None if draft is None or N == 1 else draft.data_ptr(), 0 if draft is None else draft.stride(0),
+                                  0 if draft is None else draft.stride(1), B, N, V, tokens.data_ptr(), _ptr(parents), _ptr(counts),
+                                  uniforms.data_ptr(), rows.data_ptr(), accepted.data_ptr(), next_tokens.data_ptr(), workspace.data_ptr(),
+                                  workspace.numel(), _stream())
+    _check(rc, "fgmp_verify_drafts")
+    return rows, accepted, next_tokens
