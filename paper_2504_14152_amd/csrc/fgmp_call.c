@@ -266,7 +266,8 @@ static PyObject *result(call_t *c, int rc)
     int rc = 0;                                                       \
     begin(&c, a[1]);
 
-/* (entry, types, q, k, v, cache, tree, counts, scale, max_length, out, lse, workspace, stream) */
+/* (entry, types, q, k, v, cache, tree, counts, scale, max_length, out, lse, workspace, stream); over a cache in 8 bits the entry point takes
+ * another structure's address in the cache's place, and all else alike */
 static PyObject *tree_attention(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
     ARGUMENTS(14)
@@ -393,9 +394,112 @@ static PyObject *block_norm(PyObject *self, PyObject *const *a, Py_ssize_t n)
     return result(&c, rc);
 }
 
+/* (entry, types, k, v, cache, rows, counts, lengths_out, stream) */
+static PyObject *quant_cache_append(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    ARGUMENTS(9)
+    int types = 0, type = 0, other = 0;
+    const void *const cache = cache_of(&c, a[4], &types);
+    const fgmp_heads_t k = heads(&c, a[2], "BTGD", 1 << F32 | 1 << BF16, &type), v = heads(&c, a[3], "BTGD", 1 << F32 | 1 << BF16, &other);
+    if (type != other) c.bad = 1;
+    if (a[5] == Py_None) *letter(&c, 'A') = *letter(&c, 'T');
+    const int32_t *const rows = tensor(&c, a[5], "BA", 1 << I32, NULL, NULL, 1), *const counts = tensor(&c, a[6], "B", 1 << I32, NULL, NULL, 1);
+    int32_t *const lengths = tensor(&c, a[7], "B", 1 << I32, NULL, NULL, 0);
+    void *const fn = address(&c, a[0]), *const stream = address(&c, a[8]);
+    if (!c.bad) {
+        Py_BEGIN_ALLOW_THREADS
+        rc = ((__typeof__(&fgmp_quant_cache_append))fn)(&k, &v, type == F32 ? FGMP_F32 : FGMP_BF16, *letter(&c, 'T'), cache, rows, *letter(&c, 'A'), counts,
+                                                       lengths, stream);
+        Py_END_ALLOW_THREADS
+    }
+    return result(&c, rc);
+}
+
+/* (entry, types, cache, first, k_out, v_out, stream) */
+static PyObject *quant_cache_read(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    ARGUMENTS(7)
+    int types = 0, type = 0, other = 0;
+    const void *const cache = cache_of(&c, a[2], &types);
+    const int64_t first = whole(&c, a[3]);
+    const fgmp_heads_t k = heads(&c, a[4], "BTGD", 1 << F32 | 1 << BF16, &type), v = heads(&c, a[5], "BTGD", 1 << F32 | 1 << BF16, &other);
+    /* (what does not lie within the cache is the general path's to say) */
+    if (type != other || first < 0 || first > *letter(&c, 'S') - *letter(&c, 'T')) c.bad = 1;
+    void *const fn = address(&c, a[0]), *const stream = address(&c, a[6]);
+    if (!c.bad) {
+        Py_BEGIN_ALLOW_THREADS
+        rc = ((__typeof__(&fgmp_quant_cache_read))fn)(cache, first, *letter(&c, 'T'), &k, &v, type == F32 ? FGMP_F32 : FGMP_BF16, stream);
+        Py_END_ALLOW_THREADS
+    }
+    return result(&c, rc);
+}
+
+/* (entry, types, q, k, v, positions, inv_freq, axes, q_weight, k_weight, kind, eps, interleaved, q_out, k_out, v_out, stream) */
+static PyObject *rotate_heads(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    ARGUMENTS(17)
+    static const char *const letters[3] = {"BTHD", "BTGD", "BTGD"};
+    const int either = 1 << F32 | 1 << BF16;
+    int type = 0, out_type = 0;
+    fgmp_heads_t from[3], to[3];
+    for (int i = 0; i < 3; ++i) {
+        if (a[2 + i] == Py_None) continue;
+        from[i] = heads(&c, a[2 + i], letters[i], i == 0 ? either : 1 << type, i == 0 ? &type : NULL);
+        to[i] = heads(&c, a[13 + i], letters[i], i == 0 ? either : 1 << out_type, i == 0 ? &out_type : NULL);
+    }
+    const int with_k = a[3] != Py_None, with_v = a[4] != Py_None;
+    if (a[2] == Py_None || (with_v && !with_k) || (!with_k && a[14] != Py_None) || (!with_v && a[15] != Py_None)) c.bad = 1;
+    const float *const inv_freq = tensor(&c, a[6], "P", 1 << F32, NULL, NULL, 0);
+    const int32_t *const axes = tensor(&c, a[7], "P", 1 << I32, NULL, NULL, 1);
+    const int32_t *const positions = tensor(&c, a[5], axes != NULL ? "BTX" : "BT", 1 << I32, NULL, NULL, 0);
+    const float *const q_weight = tensor(&c, a[8], "D", 1 << F32, NULL, NULL, 1), *const k_weight = tensor(&c, a[9], "D", 1 << F32, NULL, NULL, 1);
+    const int64_t kind = whole(&c, a[10]);
+    const float eps = (float)number(a[11], &c.bad);
+    const int interleaved = a[12] == Py_True;
+    if (!interleaved && a[12] != Py_False) c.bad = 1;
+    void *const fn = address(&c, a[0]), *const stream = address(&c, a[16]);
+    if (!c.bad) {
+        Py_BEGIN_ALLOW_THREADS
+        rc = ((__typeof__(&fgmp_rotate_heads))fn)(&from[0], with_k ? &from[1] : NULL, with_v ? &from[2] : NULL, type == F32 ? FGMP_F32 : FGMP_BF16, *letter(&c, 'B'),
+                                                 *letter(&c, 'T'), *letter(&c, 'H'), with_k ? *letter(&c, 'G') : 0, *letter(&c, 'D'), q_weight, k_weight,
+                                                 (fgmp_norm_t)kind, eps, positions, axes != NULL ? *letter(&c, 'X') : 1, axes, inv_freq, 2 * *letter(&c, 'P'),
+                                                 interleaved, &to[0], with_k ? &to[1] : NULL, with_v ? &to[2] : NULL, out_type == F32 ? FGMP_F32 : FGMP_BF16, stream);
+        Py_END_ALLOW_THREADS
+    }
+    return result(&c, rc);
+}
+
+/* (entry, types, target, tokens, uniforms, draft, parents, counts, rows, accepted, next, workspace, stream) */
+static PyObject *verify_drafts(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    ARGUMENTS(13)
+    int type = 0;
+    int64_t at[2] = {0, 0}, draft_at[2] = {0, 0};
+    const void *const target = tensor(&c, a[2], "BNV", 1 << F32 | 1 << BF16, &type, at, 0);
+    const int32_t *const tokens = tensor(&c, a[3], "BN", 1 << I32, NULL, NULL, 0);
+    const float *const uniforms = tensor(&c, a[4], "BN", 1 << F32, NULL, NULL, 0);
+    *letter(&c, 'M') = *letter(&c, 'N') - 1;
+    const void *const draft = tensor(&c, a[5], "BMV", 1 << type, NULL, draft_at, 1);
+    const int32_t *const parents = tensor(&c, a[6], "BN", 1 << I32, NULL, NULL, 1), *const counts = tensor(&c, a[7], "B", 1 << I32, NULL, NULL, 1);
+    int32_t *const rows = tensor(&c, a[8], "BN", 1 << I32, NULL, NULL, 0), *const accepted = tensor(&c, a[9], "B", 1 << I32, NULL, NULL, 0);
+    int32_t *const next = tensor(&c, a[10], "B", 1 << I32, NULL, NULL, 0);
+    void *const ws = tensor(&c, a[11], "W", 1 << U8, NULL, NULL, 0);
+    void *const fn = address(&c, a[0]), *const stream = address(&c, a[12]);
+    if (a[5] != Py_None && (parents != NULL || *letter(&c, 'M') == 0)) c.bad = 1;
+    if (!c.bad) {
+        Py_BEGIN_ALLOW_THREADS
+        rc = ((__typeof__(&fgmp_verify_drafts))fn)(target, type == F32 ? FGMP_F32 : FGMP_BF16, at[0], at[1], draft, draft_at[0], draft_at[1], *letter(&c, 'B'),
+                                                  *letter(&c, 'N'), *letter(&c, 'V'), tokens, parents, counts, uniforms, rows, accepted, next, ws,
+                                                  (size_t)*letter(&c, 'W'), stream);
+        Py_END_ALLOW_THREADS
+    }
+    return result(&c, rc);
+}
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(quant_gemm_fused), METHOD(tree_attention), METHOD(attention_weights), METHOD(cache_append), METHOD(cache_evict),
-                                METHOD(block_norm), {NULL, NULL, 0, NULL}};
+                                METHOD(block_norm), {"quant_cache_attention", (PyCFunction)(void (*)(void))tree_attention, METH_FASTCALL, NULL},
+                                METHOD(quant_cache_append), METHOD(quant_cache_read), METHOD(rotate_heads), METHOD(verify_drafts), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fgmp_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__fgmp_call(void)

@@ -583,16 +583,12 @@ def selftest_decode_table(fmt: int, device="cuda"):
 _TYPES = (torch.float32, torch.bfloat16, torch.int32, torch.int64, torch.uint8)
 
 
-def _not_handed(*args) -> None:
-    return None
-
-
 def _handed(name: str, *args) -> bool:
     """Whether the extension module took a call's arguments as they are (and the call went well); otherwise nothing has happened, and the
     general path has something to make, to refuse or to say."""
     if _call is None:
         return False
-    rc = getattr(_call, name, _not_handed)(lib().entries[name], _TYPES, *args, _stream())
+    rc = getattr(_call, name)(lib().entries[name], _TYPES, *args, _stream())
     if rc is None:
         return False
     if rc != 0:
