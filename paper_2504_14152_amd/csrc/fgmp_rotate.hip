@@ -5,6 +5,7 @@
 // the two halves of four pairs: a rotation stays in a lane, and a norm's sums take log2(kLanes) steps between lanes.  A workgroup has
 // one token and the heads behind each other; the token's sines and cosines are found once, by one thread for each pair, and go through LDS.
 #include <algorithm>
+#include <type_traits>
 
 #include "fgmp_cache.hpp"
 
@@ -15,7 +16,8 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256, kMaxDim = 512;
+constexpr int kThreads = 256, kMaxDim = 512, kTokensOfMany = 4;
+constexpr int64_t kMany = 1024;
 
 struct RotatePart {
     const char *from;
@@ -28,8 +30,8 @@ struct RotateArgs {
     RotatePart part[3];        // queries, keys, values
     int32_t ends[3];           // heads up to the end of each
     int32_t tokens, dim, pairs, axes, interleaved, layer;
-    uint32_t per_token;        // workgroups that share a token's heads
-    float eps;
+    uint32_t per_chunk;        // workgroups that share the heads of some tokens
+    float eps, inverse_dim;
     const int32_t *positions, *axis_of;
     const float *inv_freq;
 };
@@ -72,94 +74,152 @@ __device__ __forceinline__ void store4(char *at, int e, f32x4 x)
     else *reinterpret_cast<bf16x4 *>(at + 2 * e) = __builtin_convertvector(x, bf16x4);   // (nearest even)
 }
 
+// Sum over a vector's lanes, the same in all of them: neighbours, pairs, quads, eights change places within rows of 16 lanes, then rows and halves.
 template <int kLanes>
 __device__ __forceinline__ float head_sum(f32x4 x, f32x4 y)
 {
     float v = ((x[0] + x[1]) + (x[2] + x[3])) + ((y[0] + y[1]) + (y[2] + y[3]));
-#pragma unroll
-    for (int d = 1; d < kLanes; d <<= 1) v += __shfl_xor(v, d);
+    auto add = [&](auto control) {
+        v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xF, 0xF, true));
+    };
+    add(std::integral_constant<int, 0xB1>());                           // lane ^ 1
+    add(std::integral_constant<int, 0x4E>());                           // lane ^ 2
+    add(std::integral_constant<int, 0x141>());                          // 7 - lane of eight
+    if constexpr (kLanes >= 16) add(std::integral_constant<int, 0x140>());   // 15 - lane of a row
+    if constexpr (kLanes >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+        v = __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+    }
+    if constexpr (kLanes == 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+        v = __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+    }
     return v;
 }
 
-template <bool kFromF32, bool kToF32, int kLanes>
+// 1 / sqrt(x), off by 2^-23 of itself at most; of numbers below the normal ones, too
+__device__ __forceinline__ float inverse_root(float x)
+{
+    return x < 0x1p-100f ? __builtin_amdgcn_rsqf(x * 0x1p100f) * 0x1p50f : __builtin_amdgcn_rsqf(x);
+}
+
+template <bool kFromF32, bool kToF32, int kLanes, int kTokens>
 __global__ void __launch_bounds__(kThreads) rotate_kernel(RotateArgs a)
 {
     constexpr int kHeads = kThreads / kLanes;
-    __shared__ float2 turns[kMaxDim / 2];
-    const uint32_t token = blockIdx.x / a.per_token;
-    const int b = (int)(token / (uint32_t)a.tokens), t = (int)(token % (uint32_t)a.tokens);
-    const int lane = threadIdx.x % kLanes, first = (int)(blockIdx.x % a.per_token) * kHeads + (int)threadIdx.x / kLanes;
+    __shared__ float2 turns[kTokens][kMaxDim / 2];
+    const uint32_t chunk = blockIdx.x / a.per_chunk, chunks = ((uint32_t)a.tokens + kTokens - 1) / kTokens;
+    const int b = (int)(chunk / chunks), t = (int)(chunk % chunks) * kTokens, here = std::min(kTokens, a.tokens - t);
+    const int lane = threadIdx.x % kLanes;
+    int head = (int)(blockIdx.x % a.per_chunk) * kHeads + (int)threadIdx.x / kLanes;
+    const int step = kHeads * (int)a.per_chunk, end = a.ends[2];
     // a lane's two runs: of the rotated part, elements p .. p + 3 of its pairs' two halves, or both behind each other
     const bool there = 8 * lane < a.dim, rotated = 4 * lane < a.pairs;
     const int e0 = rotated && a.interleaved == 0 ? 4 * lane : 8 * lane, e1 = rotated && a.interleaved == 0 ? a.pairs + 4 * lane : 8 * lane + 4;
-    auto load = [&](int head, f32x4 &x, f32x4 &y) {
-        const RotatePart &p = a.part[head < a.ends[0] ? 0 : head < a.ends[1] ? 1 : 2];
-        const int h = head < a.ends[0] ? head : head < a.ends[1] ? head - a.ends[0] : head - a.ends[1];
-        const char *from = p.from + b * p.from_batch + t * p.from_token + h * p.from_head;
-        x = load4<kFromF32>(from, e0);
-        y = load4<kFromF32>(from, e1);
+    const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 x[kTokens], y[kTokens], w0 = none, w1 = none;
+    int which = 0;
+    char *to = nullptr;
+    int64_t to_token = 0;
+    auto load = [&] {
+        which = head < a.ends[0] ? 0 : head < a.ends[1] ? 1 : 2;
+        const char *from = nullptr;
+        int64_t from_token = 0;
+        const float *weight = nullptr;
+        // (a part of the arguments for each: chosen by number they would be read through memory, and every load would wait for that)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            if (which != i) continue;
+            const RotatePart &p = a.part[i];
+            const int h = head - (i == 0 ? 0 : a.ends[i - 1]);
+            from = p.from + b * p.from_batch + t * p.from_token + h * p.from_head;
+            to = p.to + b * p.to_batch + t * p.to_token + h * p.to_head;
+            from_token = p.from_token, to_token = p.to_token;
+            weight = p.weight;
+        }
+#pragma unroll
+        for (int j = 0; j < kTokens; ++j) {
+            x[j] = load4<kFromF32>(from, e0);
+            y[j] = load4<kFromF32>(from, e1);
+            if (j + 1 < here) from += from_token;    // (the last one again, where there are fewer)
+        }
+        if (weight != nullptr) {
+            w0 = *reinterpret_cast<const f32x4 *>(weight + e0);
+            w1 = *reinterpret_cast<const f32x4 *>(weight + e1);
+        }
     };
-    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
-    if (there && first < a.ends[2]) load(first, x, y);
-    for (int i = threadIdx.x; i < a.pairs; i += kThreads) {
-        const int axis = a.axis_of != nullptr ? a.axis_of[i] : 0;
-        const int32_t position = (uint32_t)axis < (uint32_t)a.axes ? a.positions[(int64_t)token * a.axes + axis] : 0;
-        turns[i] = turn(position, a.inv_freq[i]);
+#pragma unroll
+    for (int j = 0; j < kTokens; ++j) x[j] = y[j] = none;
+    if (there && head < end) load();
+    for (int i = threadIdx.x; i < kTokens * a.pairs; i += kThreads) {
+        const int j = kTokens == 1 ? 0 : i / a.pairs, pair = i - j * a.pairs;
+        const int axis = a.axis_of != nullptr ? a.axis_of[pair] : 0;
+        const int64_t token = (int64_t)b * a.tokens + t + std::min(j, here - 1);
+        const int32_t position = (uint32_t)axis < (uint32_t)a.axes ? a.positions[token * a.axes + axis] : 0;
+        turns[j][pair] = turn(position, a.inv_freq[pair]);
     }
     __syncthreads();
-    for (int head = first; head < a.ends[2]; head += kHeads * (int)a.per_token) {
-        if (head != first && there) load(head, x, y);
-        const int which = head < a.ends[0] ? 0 : head < a.ends[1] ? 1 : 2;
-        const RotatePart &p = a.part[which];
-        if (which < 2) {
-            if (p.weight != nullptr) {
+    const bool normed[2] = {a.part[0].weight != nullptr, a.part[1].weight != nullptr};
+    while (head < end) {
+        // (lanes behind a vector's end have zeros, and the part of the others)
+        const bool is_v = head >= a.ends[1], norm = !is_v && (head < a.ends[0] ? normed[0] : normed[1]);
+#pragma unroll
+        for (int j = 0; j < kTokens; ++j) {
+            if (norm) {
                 if (a.layer != 0) {
-                    const float mean = head_sum<kLanes>(x, y) / (float)a.dim;
-                    if (there) x -= mean, y -= mean;
+                    const float mean = head_sum<kLanes>(x[j], y[j]) * a.inverse_dim;
+                    if (there) x[j] -= mean, y[j] -= mean;
                 }
-                const float scale = 1.0f / __builtin_sqrtf(head_sum<kLanes>(x * x, y * y) / (float)a.dim + a.eps);
-                if (there) {
-                    x *= scale * *reinterpret_cast<const f32x4 *>(p.weight + e0);
-                    y *= scale * *reinterpret_cast<const f32x4 *>(p.weight + e1);
-                }
+                const float scale = inverse_root(head_sum<kLanes>(x[j] * x[j], y[j] * y[j]) * a.inverse_dim + a.eps);
+                x[j] *= scale * w0;
+                y[j] *= scale * w1;
             }
-            if (rotated) {
-                const float2 *c = turns + 4 * lane;
+            if (rotated && !is_v) {
+                const f32x4 t0 = *reinterpret_cast<const f32x4 *>(&turns[j][4 * lane]), t1 = *reinterpret_cast<const f32x4 *>(&turns[j][4 * lane + 2]);
+                const float c[4] = {t0[0], t0[2], t1[0], t1[2]}, s[4] = {t0[1], t0[3], t1[1], t1[3]};
                 f32x4 u, v;
                 if (a.interleaved == 0) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        u[j] = __builtin_fmaf(x[j], c[j].x, -(y[j] * c[j].y));
-                        v[j] = __builtin_fmaf(x[j], c[j].y, y[j] * c[j].x);
+                    for (int i = 0; i < 4; ++i) {
+                        u[i] = __builtin_fmaf(x[j][i], c[i], -(y[j][i] * s[i]));
+                        v[i] = __builtin_fmaf(x[j][i], s[i], y[j][i] * c[i]);
                     }
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        u[2 * j] = __builtin_fmaf(x[2 * j], c[j].x, -(x[2 * j + 1] * c[j].y));
-                        u[2 * j + 1] = __builtin_fmaf(x[2 * j], c[j].y, x[2 * j + 1] * c[j].x);
-                        v[2 * j] = __builtin_fmaf(y[2 * j], c[j + 2].x, -(y[2 * j + 1] * c[j + 2].y));
-                        v[2 * j + 1] = __builtin_fmaf(y[2 * j], c[j + 2].y, y[2 * j + 1] * c[j + 2].x);
+                    for (int i = 0; i < 2; ++i) {
+                        u[2 * i] = __builtin_fmaf(x[j][2 * i], c[i], -(x[j][2 * i + 1] * s[i]));
+                        u[2 * i + 1] = __builtin_fmaf(x[j][2 * i], s[i], x[j][2 * i + 1] * c[i]);
+                        v[2 * i] = __builtin_fmaf(y[j][2 * i], c[i + 2], -(y[j][2 * i + 1] * s[i + 2]));
+                        v[2 * i + 1] = __builtin_fmaf(y[j][2 * i], s[i + 2], y[j][2 * i + 1] * c[i + 2]);
                     }
                 }
-                x = u, y = v;
+                x[j] = u, y[j] = v;
+            }
+            if (there && j < here) {
+                store4<kToF32>(to, e0, x[j]);
+                store4<kToF32>(to, e1, y[j]);
+                to += to_token;
             }
         }
-        if (there) {
-            const int h = which == 0 ? head : head - a.ends[which - 1];
-            char *to = p.to + b * p.to_batch + t * p.to_token + h * p.to_head;
-            store4<kToF32>(to, e0, x);
-            store4<kToF32>(to, e1, y);
-        }
+        head += step;
+        if (there && head < end) load();
     }
 }
 
-template <bool kFromF32, bool kToF32>
+template <bool kFromF32, bool kToF32, int kTokens>
 void launch(const RotateArgs &a, int lanes, dim3 grid, hipStream_t st)
 {
-    if (lanes == 8) rotate_kernel<kFromF32, kToF32, 8><<<grid, kThreads, 0, st>>>(a);
-    else if (lanes == 16) rotate_kernel<kFromF32, kToF32, 16><<<grid, kThreads, 0, st>>>(a);
-    else if (lanes == 32) rotate_kernel<kFromF32, kToF32, 32><<<grid, kThreads, 0, st>>>(a);
-    else rotate_kernel<kFromF32, kToF32, 64><<<grid, kThreads, 0, st>>>(a);
+    if (lanes == 8) rotate_kernel<kFromF32, kToF32, 8, kTokens><<<grid, kThreads, 0, st>>>(a);
+    else if (lanes == 16) rotate_kernel<kFromF32, kToF32, 16, kTokens><<<grid, kThreads, 0, st>>>(a);
+    else if (lanes == 32) rotate_kernel<kFromF32, kToF32, 32, kTokens><<<grid, kThreads, 0, st>>>(a);
+    else rotate_kernel<kFromF32, kToF32, 64, kTokens><<<grid, kThreads, 0, st>>>(a);
+}
+
+template <bool kFromF32, bool kToF32>
+void launch(const RotateArgs &a, int lanes, int at_a_time, dim3 grid, hipStream_t st)
+{
+    if (at_a_time == 1) launch<kFromF32, kToF32, 1>(a, lanes, grid, st);
+    else launch<kFromF32, kToF32, kTokensOfMany>(a, lanes, grid, st);
 }
 
 }  // namespace
@@ -204,9 +264,10 @@ fgmp_status_t fgmp_rotate_heads(const fgmp_heads_t *q, const fgmp_heads_t *k, co
     }
     int lanes = 8;
     while (8 * lanes < head_dim) lanes *= 2;
-    const int64_t all = batch * tokens, turns = (end + kThreads / lanes - 1) / (kThreads / lanes);
-    a.per_token = (uint32_t)std::min<int64_t>(turns, std::max<int64_t>(1, 1024 / all));
-    if (!launch_counts(all * a.per_token, kThreads)) return FGMP_ERR_UNSUPPORTED;
+    const int at_a_time = tokens >= kTokensOfMany && batch * tokens >= kMany ? kTokensOfMany : 1;
+    const int64_t all = batch * ((tokens + at_a_time - 1) / at_a_time), turns = (end + kThreads / lanes - 1) / (kThreads / lanes);
+    a.per_chunk = (uint32_t)std::min<int64_t>(turns, std::max<int64_t>(1, 1024 / all));
+    if (!launch_counts(all * a.per_chunk, kThreads)) return FGMP_ERR_UNSUPPORTED;
     a.tokens = (int32_t)tokens;
     a.dim = (int32_t)head_dim;
     a.pairs = (int32_t)(rotary_dim / 2);
@@ -214,15 +275,16 @@ fgmp_status_t fgmp_rotate_heads(const fgmp_heads_t *q, const fgmp_heads_t *k, co
     a.interleaved = interleaved != 0;
     a.layer = kind == FGMP_NORM_LAYER;
     a.eps = eps;
+    a.inverse_dim = 1.0f / (float)head_dim;
     a.positions = positions;
     a.axis_of = axis_of;
     a.inv_freq = inv_freq;
-    const dim3 grid((unsigned)(all * a.per_token));
+    const dim3 grid((unsigned)(all * a.per_chunk));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dt == FGMP_F32 && out_dt == FGMP_F32) launch<true, true>(a, lanes, grid, st);
-    else if (dt == FGMP_F32) launch<true, false>(a, lanes, grid, st);
-    else if (out_dt == FGMP_F32) launch<false, true>(a, lanes, grid, st);
-    else launch<false, false>(a, lanes, grid, st);
+    if (dt == FGMP_F32 && out_dt == FGMP_F32) launch<true, true>(a, lanes, at_a_time, grid, st);
+    else if (dt == FGMP_F32) launch<true, false>(a, lanes, at_a_time, grid, st);
+    else if (out_dt == FGMP_F32) launch<false, true>(a, lanes, at_a_time, grid, st);
+    else launch<false, false>(a, lanes, at_a_time, grid, st);
     return hipGetLastError() == hipSuccess ? FGMP_OK : FGMP_ERR_HIP;
 }
 
