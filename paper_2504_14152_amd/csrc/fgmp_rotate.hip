@@ -16,7 +16,7 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256, kMaxDim = 512, kTokensOfMany = 4;
+constexpr int kThreads = 256, kMaxDim = 512, kTokensOfMany = 2;
 constexpr int64_t kMany = 1024;
 
 struct RotatePart {

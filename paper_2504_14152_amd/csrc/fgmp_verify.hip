@@ -4,7 +4,7 @@
 // u_t q_t(x_t) < p_r(x_t), or, for tokens that were not drawn from a distribution, u_t c < p_r(x_t), c being 1 less the probabilities of the children refused before.
 // Every workgroup of a sequence does that for itself.  Of one row, where it ends, all of the vocabulary counts: w = max(p_r - q_r, 0), or p_r without the
 // refused tokens, and the token behind is the first one up to which the sum of w exceeds u_0 times the whole sum.
-// A few dependent round trips to memory bound it (tokens, their probabilities, the row), then the row's bytes: waves add up segments of kSegment elements
+// A few dependent round trips to memory bound it (tokens, their probabilities, the row), then the row's bytes: waves add up segments of 64 kRows elements
 // each, one of the workgroup that is the last of its sequence finds the segment, and in it the element.  Up to 64 tokens each wave does the
 // walk in its own lanes.  Sums are of 64 bits: in 32, those over a vocabulary are off by more than many a token's probability.
 #include <algorithm>
@@ -16,8 +16,11 @@ namespace fgmp {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64, kRows = 16, kSegment = 64 * kRows;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMaxTokens = 1024, kFewTokens = 64;
+// Rows of 64 elements in a segment.  Short ones where the chip holds all their waves at a time, long ones else: one sequence of 32000, 4 / 8 / 16 rows: 7.5 / 7.5 / 10.4
+// us; 32 sequences of 2 x 151937: 19.9 / 13.7 / 13.1.
+constexpr int kShortRows = 8, kLongRows = 16, kWavesAtATime = 4096;
 constexpr int kHeld = 8;           // sums of segments that a lane keeps in registers
 constexpr int64_t kMaxVocab = (int64_t)1 << 24, kMaxBatch = 16384;
 
@@ -202,9 +205,10 @@ __device__ __forceinline__ Walk walk_of_many(const VerifyArgs &a, int b, ManyTok
 }
 
 // Weights of a segment's elements: w[r] that of element kSegment * segment + 64 r + lane.  `whole`: the row as it is, nothing taken from it.
-template <bool kF32, bool kFew, typename Tokens>
+template <bool kF32, bool kFew, int kRows, typename Tokens>
 __device__ __forceinline__ void weights_of(const VerifyArgs &a, int b, int segment, const Walk &walk, const Tokens &s, bool whole, double *w)
 {
+    constexpr int kSegment = 64 * kRows;
     const int lane = threadIdx.x & 63, first = segment * kSegment + lane;
     const char *target = a.target + b * a.target_batch + walk.last * a.target_row;
     const bool refused = !whole && (kFew ? walk.refused_lanes != 0ull : walk.refused != 0);
@@ -241,11 +245,11 @@ __device__ __forceinline__ void weights_of(const VerifyArgs &a, int b, int segme
     }
 }
 
-template <bool kF32, bool kFew, typename Tokens>
+template <bool kF32, bool kFew, int kRows, typename Tokens>
 __device__ __forceinline__ double segment_sum(const VerifyArgs &a, int b, int segment, const Walk &walk, const Tokens &s, bool whole)
 {
     double w[kRows];
-    weights_of<kF32, kFew>(a, b, segment, walk, s, whole, w);
+    weights_of<kF32, kFew, kRows>(a, b, segment, walk, s, whole, w);
     double sum[4] = {w[0], w[1], w[2], w[3]};
 #pragma unroll
     for (int r = 4; r < kRows; ++r) sum[r % 4] += w[r];
@@ -253,7 +257,7 @@ __device__ __forceinline__ double segment_sum(const VerifyArgs &a, int b, int se
 }
 
 // The token behind, by the sums of the segments; -1 where they are all nothing.  For one wave.
-template <bool kF32, bool kFew, typename Tokens, typename Sum>
+template <bool kF32, bool kFew, int kRows, typename Tokens, typename Sum>
 __device__ __forceinline__ int32_t pick(const VerifyArgs &a, int b, const Walk &walk, const Tokens &s, bool whole, float u0, Sum sum_at)
 {
     const int lane = threadIdx.x & 63;
@@ -287,7 +291,7 @@ __device__ __forceinline__ int32_t pick(const VerifyArgs &a, int b, const Walk &
     const double rest = in_lane - of_lane(found >= 0 ? before : before_last, owner);
     // the row of 64 elements, then the element
     double w[kRows];
-    weights_of<kF32, kFew>(a, b, segment, walk, s, whole, w);
+    weights_of<kF32, kFew, kRows>(a, b, segment, walk, s, whole, w);
     double up_to = 0.0, before_row = 0.0, x = w[0];
     int row = -1, last_row = 0;
 #pragma unroll
@@ -303,10 +307,10 @@ __device__ __forceinline__ int32_t pick(const VerifyArgs &a, int b, const Walk &
     for (int r = 1; r < kRows; ++r) x = row == r ? w[r] : x;
     const double scan = wave_scan(x);
     const uint64_t here = __ballot(x > 0.0 && before_row + scan > rest), any = __ballot(x > 0.0);
-    return kSegment * segment + 64 * row + (in_row && here != 0ull ? __builtin_ctzll(here) : 63 - __builtin_clzll(any));
+    return 64 * kRows * segment + 64 * row + (in_row && here != 0ull ? __builtin_ctzll(here) : 63 - __builtin_clzll(any));
 }
 
-template <bool kF32, bool kFew>
+template <bool kF32, bool kFew, int kRows>
 __global__ void __launch_bounds__(kThreads) verify_kernel(VerifyArgs a)
 {
     __shared__ std::conditional_t<kFew, NoTokens, ManyTokens> s;
@@ -322,7 +326,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(VerifyArgs a)
     double *const sums = a.sums + (int64_t)b * a.segments;
     if (walk.count > 0) {
         for (int segment = part * kWaves + wave; segment < a.segments; segment += (int)a.workgroups * kWaves) {
-            const double sum = segment_sum<kF32, kFew>(a, b, segment, walk, s, false);
+            const double sum = segment_sum<kF32, kFew, kRows>(a, b, segment, walk, s, false);
             if (lane == 0) {
                 if (one) own_sums[segment] = sum;
                 else store_sum(&sums[segment], sum);
@@ -360,7 +364,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(VerifyArgs a)
     }
     auto sum_at = [&](int i) { return one ? own_sums[i] : load_sum(&sums[i]); };
     if (wave == 0) {
-        const int32_t token = pick<kF32, kFew>(a, b, walk, s, false, u0, sum_at);
+        const int32_t token = pick<kF32, kFew, kRows>(a, b, walk, s, false, u0, sum_at);
         if (lane == 0) {
             nothing = token < 0;
             if (token >= 0) a.next[b] = token;
@@ -370,7 +374,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(VerifyArgs a)
     if (!nothing) return;
     // nothing is left of the row by rounding alone (or the row is all zeros): the row as it is
     for (int segment = wave; segment < a.segments; segment += kWaves) {
-        const double sum = segment_sum<kF32, kFew>(a, b, segment, walk, s, true);
+        const double sum = segment_sum<kF32, kFew, kRows>(a, b, segment, walk, s, true);
         if (lane == 0) {
             if (one) own_sums[segment] = sum;
             else store_sum(&sums[segment], sum);
@@ -379,16 +383,23 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(VerifyArgs a)
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (wave == 0) {
-        const int32_t token = pick<kF32, kFew>(a, b, walk, s, true, u0, sum_at);
+        const int32_t token = pick<kF32, kFew, kRows>(a, b, walk, s, true, u0, sum_at);
         if (lane == 0) a.next[b] = token;
     }
 }
 
-template <bool kF32>
+template <bool kF32, int kRows>
 void launch(const VerifyArgs &a, dim3 grid, hipStream_t st)
 {
-    if (a.n <= kFewTokens) verify_kernel<kF32, true><<<grid, kThreads, 0, st>>>(a);
-    else verify_kernel<kF32, false><<<grid, kThreads, 0, st>>>(a);
+    if (a.n <= kFewTokens) verify_kernel<kF32, true, kRows><<<grid, kThreads, 0, st>>>(a);
+    else verify_kernel<kF32, false, kRows><<<grid, kThreads, 0, st>>>(a);
+}
+
+template <bool kF32>
+void launch(const VerifyArgs &a, int rows, dim3 grid, hipStream_t st)
+{
+    if (rows == kShortRows) launch<kF32, kShortRows>(a, grid, st);
+    else launch<kF32, kLongRows>(a, grid, st);
 }
 
 }  // namespace
@@ -402,7 +413,7 @@ extern "C" {
 size_t fgmp_verify_drafts_workspace_bytes(int64_t batch, int64_t tokens, int64_t vocab)
 {
     if (batch <= 0 || batch > kMaxBatch || tokens <= 0 || tokens > kMaxTokens || vocab <= 0 || vocab > kMaxVocab) return 0;
-    return kWsCtrlRegion + (size_t)(batch * ((vocab + kSegment - 1) / kSegment)) * sizeof(double);
+    return kWsCtrlRegion + (size_t)(batch * ((vocab + 64 * kShortRows - 1) / (64 * kShortRows))) * sizeof(double);
 }
 
 fgmp_status_t fgmp_verify_drafts(const void *target, fgmp_dtype_t dt, int64_t target_batch_stride, int64_t target_row_stride, const void *draft,
@@ -443,7 +454,9 @@ fgmp_status_t fgmp_verify_drafts(const void *target, fgmp_dtype_t dt, int64_t ta
     a.next = next;
     a.n = (int32_t)tokens;
     a.vocab = (int32_t)vocab;
-    a.segments = (int32_t)((vocab + kSegment - 1) / kSegment);
+    const int64_t short_segments = (vocab + 64 * kShortRows - 1) / (64 * kShortRows);
+    const int row_count = batch * short_segments <= kWavesAtATime ? kShortRows : kLongRows;
+    a.segments = (int32_t)((vocab + 64 * row_count - 1) / (64 * row_count));
     a.counter_shift = batch <= 1024 ? 4u : 0u;   // (lines of their own, where the control region has room)
     a.counters = static_cast<uint32_t *>(workspace);
     a.sums = reinterpret_cast<double *>(static_cast<char *>(workspace) + kWsCtrlRegion);
@@ -451,8 +464,8 @@ fgmp_status_t fgmp_verify_drafts(const void *target, fgmp_dtype_t dt, int64_t ta
     a.workgroups = (uint32_t)std::min<int64_t>(most, std::max<int64_t>(2, 8192 / batch));
     const dim3 grid((unsigned)(batch * a.workgroups));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dt == FGMP_F32) launch<true>(a, grid, st);
-    else launch<false>(a, grid, st);
+    if (dt == FGMP_F32) launch<true>(a, row_count, grid, st);
+    else launch<false>(a, row_count, grid, st);
     return hipGetLastError() == hipSuccess ? FGMP_OK : FGMP_ERR_HIP;
 }
 
