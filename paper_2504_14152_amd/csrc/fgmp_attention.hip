@@ -15,7 +15,7 @@ namespace fgmp {
 
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kFewWaves = 4, kManyWaves = 8;   // of a workgroup
 constexpr int kMaxTokens = 1024;
 
 template <bool kF32>
@@ -289,7 +289,7 @@ __device__ __forceinline__ void add_non_finite(RowState<kDim> &st, const f32x4 *
 // kRows: groups of 16 rows that a workgroup's waves hold, every wave all of them.  A tile of keys and values is asked for while the one
 // before is worked on: the keys as soon as its scores are there, the values as soon as they have changed places.
 // kEight: a cache in 8 bits, all else BF16; codes become BF16 when their tile is worked on.
-template <bool kF32, int kDim, int kRows, bool kEight = false>
+template <bool kF32, int kDim, int kRows, bool kEight = false, int kWaves = kFewWaves>
 __global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(ArgsOf<kEight> a)
 {
     static_assert(!(kF32 && kEight), "new tokens, results and weights are BF16 where the cache is in 8 bits");
@@ -541,8 +541,9 @@ __global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(
         const int64_t at = ((int64_t)b * a.tokens + t) * a.q_heads + head;   // (of rows that exist)
         const float inverse = inverse_sum(l);
 #pragma unroll
-        for (int m4 = 0; m4 < kPer / kWaves; ++m4) {
-            const int m = wave * (kPer / kWaves) + m4;
+        for (int m4 = 0; m4 < (kPer + kWaves - 1) / kWaves; ++m4) {
+            const int m = kPer < kWaves ? wave : wave * (kPer / kWaves) + m4;
+            if (kPer < kWaves && wave >= kPer) continue;
             f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) o += *reinterpret_cast<const f32x4 *>(&merge_o[w][((r * kPer + m) * 64 + lane) * 4]) * f[w];
@@ -667,9 +668,9 @@ struct WeightArgs {
 };
 
 template <bool kF32, int kDim>
-__global__ void __launch_bounds__(64 * kWaves) weights_kernel(WeightArgs a)
+__global__ void __launch_bounds__(64 * kFewWaves) weights_kernel(WeightArgs a)
 {
-    constexpr int kPieces = Operand<kF32, kDim>::kPieces, kBlock = 16 * kWeightKeys * kWaves;
+    constexpr int kPieces = Operand<kF32, kDim>::kPieces, kBlock = 16 * kWeightKeys * kFewWaves;
     __shared__ u32x4 stage[kStage / 16][kPieces][64];
     __shared__ float stage_lse[kStage];   // log2 of the row's sum; +inf: a row that adds nothing
     __shared__ int32_t stage_end[kStage]; // slots that the row sees
@@ -685,7 +686,7 @@ __global__ void __launch_bounds__(64 * kWaves) weights_kernel(WeightArgs a)
     const int rows = count * a.group;
     // rows start .. start + kStage - 1; of those that there are not, whole groups of 16 are left as they are
     auto put = [&](int start) {
-        for (int p = tid; p < kStage / 16 * kPieces * 64; p += 64 * kWaves) {
+        for (int p = tid; p < kStage / 16 * kPieces * 64; p += 64 * kFewWaves) {
             if (start + p / (kPieces * 64) * 16 >= rows) break;
             const int r = start + p / (kPieces * 64) * 16 + (p & 15);
             u32x4 x = {0u, 0u, 0u, 0u};
@@ -773,12 +774,13 @@ __global__ void __launch_bounds__(64 * kWaves) weights_kernel(WeightArgs a)
 struct AttendPlan {
     int waves_of_rows;      // of the kernel for many rows; 0: the other one
     int row_groups;         // groups of 16 rows, of the other one
+    int waves;              // of a workgroup of the other one
     int tile_keys, min_tiles;
     int64_t row_blocks, splits;
     int64_t units, workgroups;   // ranges of all heads and sequences; in eights, and for each row block
 };
 
-AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t heads, int64_t head_dim, bool f32, int64_t max_length)
+AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t heads, int64_t head_dim, bool f32, int64_t max_length, bool eight = false)
 {
     AttendPlan p = {};
     const int64_t groups = (tokens * (q_heads / heads) + 15) / 16;
@@ -804,6 +806,10 @@ AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t h
     }
     const int64_t whole = batch * heads * p.row_blocks, least = (int64_t)p.tile_keys * p.min_tiles;
     p.splits = std::max<int64_t>(1, std::min((max_length + least - 1) / least, (want + whole - 1) / whole));
+    p.waves = kFewWaves;
+    // A short cache in 8 bits is not cut: twice the waves, and no launch to join.  One sequence's 32 heads of 517 / 1024 / 2048 slots, cut / not: 11.8 / 9.8, 13.1 / 12.9,
+    // 16.8 / 21.7 us; 8 x 8 heads 13.2 / 10.4, 16.5 / 14.7, 25.1 / 21.9, of 4096 29.9 / 36.4 (head_dim 256 has no registers for so many waves)
+    if (eight && p.row_groups == 1 && head_dim != 256 && p.splits > 1 && max_length <= (whole >= 64 ? 2048 : 1024)) p.splits = 1, p.waves = kManyWaves;
     p.units = batch * heads * p.splits;
     p.workgroups = (p.units + 7) / 8 * 8 * p.row_blocks;
     return p;
@@ -819,9 +825,13 @@ void attend_launch(const ArgsOf<kEight> &a, const AttendPlan &p, hipStream_t st)
 {
     const dim3 grid((unsigned)p.workgroups);
     if (p.waves_of_rows > 0) attend_wide(a, p.waves_of_rows, (uint32_t)p.workgroups, st);
-    else if (p.row_groups == 1) attend_kernel<kF32, kDim, 1, kEight><<<grid, 64 * kWaves, 0, st>>>(a);
+    else if (p.row_groups == 1 && (!kEight || p.waves == kFewWaves)) attend_kernel<kF32, kDim, 1, kEight><<<grid, 64 * kFewWaves, 0, st>>>(a);
+    if constexpr (kEight) {
+        if constexpr (kDim != 256)
+            if (p.row_groups == 1 && p.waves == kManyWaves) attend_kernel<kF32, kDim, 1, kEight, kManyWaves><<<grid, 64 * kManyWaves, 0, st>>>(a);
+    }
     if constexpr (kDim != 256) {
-        if (p.row_groups == 2) attend_kernel<kF32, kDim, 2, kEight><<<grid, 64 * kWaves, 0, st>>>(a);
+        if (p.row_groups == 2) attend_kernel<kF32, kDim, 2, kEight><<<grid, 64 * kFewWaves, 0, st>>>(a);
     }
     const int64_t rows = (int64_t)a.c.batch * a.tokens * a.q_heads;
     if (p.splits > 16) join_kernel<kF32, kDim, 4><<<dim3((unsigned)rows), 256, 0, st>>>(a, rows);
@@ -853,7 +863,7 @@ static fgmp_status_t attend(ArgsOf<kEight> &a, fgmp_dtype_t dtype, const fgmp_he
         if ((rc = check_heads(v, a.c.batch, tokens, a.c.heads, dim, size, false)) != FGMP_OK) return rc;
     }
     if (max_length == 0 || max_length > a.c.slots) max_length = a.c.slots;
-    const AttendPlan p = attend_plan(a.c.batch, tokens, q_heads, a.c.heads, dim, dtype == FGMP_F32, max_length);
+    const AttendPlan p = attend_plan(a.c.batch, tokens, q_heads, a.c.heads, dim, dtype == FGMP_F32, max_length, kEight);
     const int64_t rows = a.c.batch * tokens * q_heads;
     const size_t need = attend_bytes(p, rows, dim);
     if (need > 0) {
@@ -862,7 +872,7 @@ static fgmp_status_t attend(ArgsOf<kEight> &a, fgmp_dtype_t dtype, const fgmp_he
         if (workspace_bytes < need) return FGMP_ERR_BUFFER_TOO_SMALL;
     }
     // (ranges are joined only where heads and row blocks are fewer than 1024, of 256 rows at most: that launch stays small)
-    if (!launch_counts(p.workgroups, 64 * (p.waves_of_rows > 0 ? p.waves_of_rows : kWaves)) || rows >= (int64_t)1 << 31) return FGMP_ERR_UNSUPPORTED;
+    if (!launch_counts(p.workgroups, 64 * (p.waves_of_rows > 0 ? p.waves_of_rows : p.waves)) || rows >= (int64_t)1 << 31) return FGMP_ERR_UNSUPPORTED;
     a.q = static_cast<const char *>(q->data);
     a.q_batch = q->batch_stride * size, a.q_token = q->token_stride * size, a.q_head = q->head_stride * size;
     a.out = static_cast<char *>(out->data);
@@ -958,10 +968,10 @@ fgmp_status_t fgmp_attention_weights(const fgmp_heads_t *q, const float *lse, in
     const int size = dtype_size(cache->dtype), dim = a.c.head_dim;
     if ((rc = check_heads(q, a.c.batch, tokens, q_heads, dim, size, false)) != FGMP_OK) return rc;
     if (max_length == 0 || max_length > a.c.slots) max_length = a.c.slots;
-    constexpr int kBlock = 16 * kWeightKeys * kWaves;
+    constexpr int kBlock = 16 * kWeightKeys * kFewWaves;
     const int64_t pairs = (int64_t)a.c.batch * a.c.heads;
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>((max_length + kBlock - 1) / kBlock, (kWeightWorkgroups + pairs - 1) / pairs));
-    if (!launch_counts(pairs * blocks, 64 * kWaves)) return FGMP_ERR_UNSUPPORTED;
+    if (!launch_counts(pairs * blocks, 64 * kFewWaves)) return FGMP_ERR_UNSUPPORTED;
     a.q = static_cast<const char *>(q->data);
     a.q_batch = q->batch_stride * size, a.q_token = q->token_stride * size, a.q_head = q->head_stride * size;
     a.lse = lse;
@@ -979,13 +989,13 @@ fgmp_status_t fgmp_attention_weights(const fgmp_heads_t *q, const float *lse, in
     const dim3 grid((unsigned)(pairs * blocks));
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (cache->dtype == FGMP_F32) {
-        if (dim == 64) weights_kernel<true, 64><<<grid, 64 * kWaves, 0, st>>>(a);
-        else if (dim == 128) weights_kernel<true, 128><<<grid, 64 * kWaves, 0, st>>>(a);
-        else weights_kernel<true, 256><<<grid, 64 * kWaves, 0, st>>>(a);
+        if (dim == 64) weights_kernel<true, 64><<<grid, 64 * kFewWaves, 0, st>>>(a);
+        else if (dim == 128) weights_kernel<true, 128><<<grid, 64 * kFewWaves, 0, st>>>(a);
+        else weights_kernel<true, 256><<<grid, 64 * kFewWaves, 0, st>>>(a);
     } else {
-        if (dim == 64) weights_kernel<false, 64><<<grid, 64 * kWaves, 0, st>>>(a);
-        else if (dim == 128) weights_kernel<false, 128><<<grid, 64 * kWaves, 0, st>>>(a);
-        else weights_kernel<false, 256><<<grid, 64 * kWaves, 0, st>>>(a);
+        if (dim == 64) weights_kernel<false, 64><<<grid, 64 * kFewWaves, 0, st>>>(a);
+        else if (dim == 128) weights_kernel<false, 128><<<grid, 64 * kFewWaves, 0, st>>>(a);
+        else weights_kernel<false, 256><<<grid, 64 * kFewWaves, 0, st>>>(a);
     }
     return hipGetLastError() == hipSuccess ? FGMP_OK : FGMP_ERR_HIP;
 }
