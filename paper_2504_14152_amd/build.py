@@ -23,6 +23,9 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "fgmp.h")
 CALL_SOURCE = os.path.join(CSRC, "fgmp_call.c")
 # what the binding hands the fused call's arguments over with; the name says for which interpreter
 CALL = os.path.join(HERE, "_fgmp_call" + sysconfig.get_config_var("EXT_SUFFIX"))
+# what that module looks into tensors with; for this interpreter and its torch
+TENSORS_SOURCE = os.path.join(CSRC, "fgmp_tensors.cpp")
+TENSORS = os.path.join(HERE, "_fgmp_tensors" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["fgmp_quantize.hip", "fgmp_gemm.hip", "fgmp_gemm_skinny.hip", "fgmp_gemm_stream.hip", "fgmp_gemm_mid.hip",
            "fgmp_gemm_mixed.hip",
            "fgmp_select.hip", "fgmp_attention.hip", "fgmp_attention_wide.hip", "fgmp_cache.hip",
@@ -54,6 +57,10 @@ def is_stale(path: str) -> bool:
 def call_is_stale() -> bool:
     """The extension module is compiled with the header, too: argument lists, structures and codes are its."""
     return not os.path.exists(CALL) or any(os.path.getmtime(f) > os.path.getmtime(CALL) for f in (CALL_SOURCE, HEADER))
+
+
+def tensors_are_stale() -> bool:
+    return not os.path.exists(TENSORS) or os.path.getmtime(TENSORS_SOURCE) > os.path.getmtime(TENSORS)
 
 
 def _hipcc() -> str:
@@ -93,19 +100,33 @@ def build_one(variant: str | None = None, verbose: bool = False, extra_flags: li
 
 
 def build_call() -> str:
-    """The extension module for the interpreter that runs this.  Moved to its place when it is whole: other processes may look for it
-    there, or build it, too."""
-    part = f"{CALL}.{os.getpid()}"
-    cmd = [os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"], CALL_SOURCE, "-o", part]
+    """The extension module for the interpreter that runs this."""
+    return _in_place(CALL, [os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"], CALL_SOURCE])
+
+
+def build_tensors() -> str:
+    """What it looks into tensors with, for the torch that runs here."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    include = os.path.join(root, "include")
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I" + sysconfig.get_paths()["include"], "-I" + include, "-I" + os.path.join(include, "torch", "csrc", "api", "include"), TENSORS_SOURCE,
+           "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    return _in_place(TENSORS, cmd)
+
+
+def _in_place(path: str, cmd: list[str]) -> str:
+    """What `cmd` makes, moved to its place when it is whole: other processes may look for it there, or build it, too."""
+    part = f"{path}.{os.getpid()}"
     try:
-        res = subprocess.run(cmd, capture_output=True, text=True)
+        res = subprocess.run(cmd + ["-o", part], capture_output=True, text=True)
         if res.returncode != 0:
-            raise RuntimeError(f"{cmd[0]} failed for {CALL_SOURCE}:\n{res.stderr}")
-        os.replace(part, CALL)
+            raise RuntimeError(f"{cmd[0]} failed for {os.path.basename(path)}:\n{res.stderr}")
+        os.replace(part, path)
     finally:
         if os.path.exists(part):
             os.remove(part)
-    return CALL
+    return path
 
 
 def build(verbose: bool = False, extra_flags: list[str] | None = None, out: str | None = None,
@@ -116,6 +137,10 @@ def build(verbose: bool = False, extra_flags: list[str] | None = None, out: str 
     path = build_one(None, verbose, extra_flags, out)
     if extension:
         build_call()
+        try:
+            build_tensors()
+        except RuntimeError as e:   # (calls take a little longer without it)
+            print(e, file=sys.stderr)
     if out is None and variants:
         for v in VARIANTS:
             build_one(v, verbose, extra_flags)

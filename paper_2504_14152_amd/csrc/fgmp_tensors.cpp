@@ -1,0 +1,37 @@
+/* What the extension module asks of a torch tensor, taken from its C++ object: the same facts as its Python attributes and methods give, without
+ * building Python objects for them.  One tensor: 0.27 us through attributes, 0.02 here (a call of eleven: 3 us of the 7.4 it took).
+ * Compiled with torch's headers and loaded beside the extension module where both belong to the torch that runs; without it the attributes are asked.
+ */
+#include <torch/csrc/autograd/python_variable.h>
+#include <torch/version.h>
+
+extern "C" {
+
+const char *fgmp_tensors_torch(void) { return TORCH_VERSION; }
+
+/* Dimensions of a plain tensor on the GPU (not of a subclass, which may answer for itself), up to `most`, with its sizes, strides, address and type: 0
+ * float32, 1 bfloat16, 2 int32, 3 int64, 4 uint8, -1 another.  -1: nothing is said about `o`. */
+int fgmp_tensors_look(PyObject *o, int most, int64_t *sizes, int64_t *strides, int *type, void **data)
+{
+    if (!THPVariable_CheckExact(o)) return -1;
+    try {
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || t.layout() != at::kStrided || t.dim() > most) return -1;
+        const int n = (int)t.dim();
+        for (int i = 0; i < n; ++i) sizes[i] = t.size(i), strides[i] = t.stride(i);
+        switch (t.scalar_type()) {
+        case at::kFloat: *type = 0; break;
+        case at::kBFloat16: *type = 1; break;
+        case at::kInt: *type = 2; break;
+        case at::kLong: *type = 3; break;
+        case at::kByte: *type = 4; break;
+        default: *type = -1;
+        }
+        *data = t.data_ptr();
+        return n;
+    } catch (...) {
+        return -1;   /* (the attributes say what is wrong) */
+    }
+}
+
+}  /* extern "C" */

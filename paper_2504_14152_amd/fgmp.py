@@ -95,7 +95,23 @@ def _load_call():
         loader.exec_module(module)
     except (ImportError, OSError, RuntimeError):
         return None
+    _load_tensors(module)
     return module
+
+
+def _load_tensors(module) -> None:
+    """Gives the extension module its way into tensors' C++ objects, where that is compiled for the torch that runs; it asks their attributes
+    otherwise."""
+    try:
+        if _build.tensors_are_stale():
+            _build.build_tensors()
+        tensors = ctypes.PyDLL(_build.TENSORS)
+        tensors.fgmp_tensors_torch.restype = ctypes.c_char_p
+        if tensors.fgmp_tensors_torch().decode() != torch.__version__.split("+")[0]:
+            return
+        module.look_into_tensors(ctypes.cast(tensors.fgmp_tensors_look, ctypes.c_void_p).value)
+    except (OSError, RuntimeError, AttributeError):
+        pass
 
 
 class use_library:

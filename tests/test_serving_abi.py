@@ -68,8 +68,9 @@ def test_attention_over_8_bits_refuses():
     assert _attend(q_heads=5) == SHAPE and _attend(tokens=1025) == UNSUPPORTED
     assert _attend(q=_heads(None)) == INVALID and _attend(q=_heads(AT + 8)) == ALIGN and _attend(q=_heads(strides=(1024, 516, 128))) == ALIGN
     assert _attend(out=_heads(strides=(1024, 0, 128))) == SHAPE and _attend(k=_heads(AT + 8)) == ALIGN
-    need = fgmp.tree_attention_workspace_bytes(2, 2, 4, 2, 128, 256)
-    assert _attend(ws_n=need - 1) == SMALL and _attend(ws=None) == INVALID and _attend(ws=AT + 4) == ALIGN
+    long = _quant(pages_per_sequence=64, table_stride=64)
+    need = fgmp.tree_attention_workspace_bytes(2, 2, 4, 2, 128, 64 * 64)
+    assert _attend(cache=long, ws_n=need - 1) == SMALL and _attend(cache=long, ws=None) == INVALID and _attend(cache=long, ws=AT + 4) == ALIGN
     assert _attend(cache=_quant(batch=MANY, heads=257), tokens=1, q_heads=257, max_length=1) == UNSUPPORTED
 
 
@@ -280,3 +281,46 @@ def test_the_extension_counts_its_arguments(name, count):
     with pytest.raises(TypeError):
         f(*[None] * (count - 1))
     assert f(*[None] * count) is None and f(0, (1, 2), *[None] * (count - 2)) is None
+
+
+def test_tensors_are_looked_into_where_that_was_compiled_for_this_torch(monkeypatch, tmp_path):
+    """The way into a tensor's C++ object is taken for the torch it was compiled for alone; plain tensors of the CPU, subclasses and objects that are
+    no tensors are left to their attributes."""
+    from paper_2504_14152_amd import build
+    fgmp.lib()
+    tensors = ctypes.PyDLL(build.TENSORS)
+    tensors.fgmp_tensors_torch.restype = ctypes.c_char_p
+    assert tensors.fgmp_tensors_torch().decode() == torch.__version__.split("+")[0]
+    sizes, strides, kind, data = (I64 * 4)(), (I64 * 4)(), I(), VP()
+    look = tensors.fgmp_tensors_look
+    look.argtypes = [ctypes.py_object, I, ctypes.POINTER(I64), ctypes.POINTER(I64), ctypes.POINTER(I), ctypes.POINTER(VP)]
+    for o in (torch.zeros(3), _gpu(torch.zeros(3)), _t(16, 3), None, 7):
+        assert look(o, 4, sizes, strides, ctypes.byref(kind), ctypes.byref(data)) == -1
+    told = []
+    module = type("Module", (), {"look_into_tensors": staticmethod(told.append)})
+    fgmp._load_tensors(module)
+    assert len(told) == 1 and told[0]
+    monkeypatch.setattr(torch, "__version__", "9.9.9")
+    fgmp._load_tensors(module)
+    monkeypatch.undo()
+    monkeypatch.setattr(build, "TENSORS", str(tmp_path / "none.so"))
+    monkeypatch.setenv("CXX", str(tmp_path / "no-compiler"))
+    fgmp._load_tensors(module)          # (nothing to compile with)
+    assert len(told) == 1
+
+
+@pytest.mark.gpu
+def test_a_tensor_says_the_same_either_way():
+    from paper_2504_14152_amd import build
+    tensors = ctypes.PyDLL(build.TENSORS)
+    sizes, strides, kind, data = (I64 * 4)(), (I64 * 4)(), I(), VP()
+    look = tensors.fgmp_tensors_look
+    look.argtypes = [ctypes.py_object, I, ctypes.POINTER(I64), ctypes.POINTER(I64), ctypes.POINTER(I), ctypes.POINTER(VP)]
+    base = torch.zeros(4, 6, 8, 10, device="cuda")
+    for t in (base, base[1:, ::2], base.transpose(1, 2), base[0, 0, 0], base[:0], base.bfloat16(), base.int(), base.long(), base.byte(), base.half(), base[..., 3],
+              base[:1].expand(9, 6, 8, 10), torch.nn.Parameter(base)):
+        n = look(t, 4, sizes, strides, ctypes.byref(kind), ctypes.byref(data))
+        types = {torch.float32: 0, torch.bfloat16: 1, torch.int32: 2, torch.int64: 3, torch.uint8: 4}
+        assert n == t.dim() and tuple(sizes[:n]) == t.shape and tuple(strides[:n]) == t.stride() and kind.value == types.get(t.dtype, -1)
+        assert (data.value or 0) == t.data_ptr()
+    assert look(base[None], 4, sizes, strides, ctypes.byref(kind), ctypes.byref(data)) == -1
