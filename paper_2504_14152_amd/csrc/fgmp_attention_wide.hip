@@ -68,7 +68,10 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
     constexpr int kThreads = 64 * kWaves, kPieces = kDim / 8, kBlocks = kDim / 32, kSteps = kDim / 16;
     // loads of a thread: kKeyLoads pieces of keys, kKeyRows rows apart; and of values, kRounds times four keys x 2 kWords elements, of which
     // kQuadThreads threads have a row
-    constexpr int kKeyLoads = kKeys * kPieces / kThreads, kKeyRows = kThreads / kPieces;
+    // (codes: 16 to a load, where that is work for all threads)
+    constexpr int kKeyCodes = kEight && kKeys * (kDim / 16) >= kThreads ? 16 : 8;
+    constexpr int kKeyThreads = kDim / kKeyCodes, kKeyLoads = kKeys * kKeyThreads / kThreads, kKeyRows = kThreads / kKeyThreads;
+    constexpr int kNewLoads = kKeys * kPieces / kThreads, kNewRows = kThreads / kPieces;
     constexpr int kWords = kWaves == 8 ? kDim / 64 : kDim == 256 ? 4 : kDim / 32, kQuadThreads = kDim / (2 * kWords), kQuads = kThreads / kQuadThreads;
     constexpr int kRounds = kKeys / 4 / kQuads;
     __shared__ Tile<kDim> buffer[2];
@@ -93,15 +96,15 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
     // ---- a tile on its way: global memory -> registers -> LDS ----
     const uint32_t step = (uint32_t)a.c.token_stride;
     constexpr int kSize = kEight ? 1 : 2, kRaw = kEight ? (kWords + 1) / 2 : kWords;   // of a cached element; words that hold a thread's values of a key
-    const int key_row = tid / kPieces, key_at = tid % kPieces * (8 * kSize), quad = tid / kQuadThreads, value_at = tid % kQuadThreads * (2 * kWords * kSize);
+    const int key_row = tid / kKeyThreads, key_at = tid % kKeyThreads * (kKeyCodes * kSize), quad = tid / kQuadThreads, value_at = tid % kQuadThreads * (2 * kWords * kSize);
     // (the even tiles in one set of registers, the odd ones in the other: room for two tiles on their way)
-    typedef std::conditional_t<kEight, u32x2, u32x4> Piece;
+    typedef std::conditional_t<kEight && kKeyCodes == 8, u32x2, u32x4> Piece;
     Piece key[2][kKeyLoads];
     uint32_t value[2][kRounds][4][kRaw];
     uint32_t key_scale[2][kEight ? kKeyLoads : 1], value_scale[2][kEight ? kRounds : 1];   // (a byte; a byte for each of four keys)
     // A wave's loads of one kind and round are of one group of 16 slots, whose page is looked up a tile ahead of the load.
     uint32_t key_page[kKeyLoads], value_page[kRounds], key_first[kKeyLoads], value_first[kRounds];
-    const int key_group = wave * (64 / kPieces), value_group = wave * (64 / kQuadThreads);   // (in rows, and in quads)
+    const int key_group = wave * (64 / kKeyThreads), value_group = wave * (64 / kQuadThreads);   // (in rows, and in quads)
     const uint32_t last_group = (uint32_t)(n - 1) / 16u;     // (used where there are slots)
     auto look_up = [&](int tile) {
         const uint32_t u = (uint32_t)(begin + tile) * kGroups;
@@ -159,9 +162,7 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
         }
     };
     // `left`: keys of the tile that there are; what lies behind them must not meet a weight of zero: it might not be finite
-    auto put = [&](Tile<kDim> &to, u32x4 *keys, uint32_t (*values)[4][kWords], int left) {
-#pragma unroll
-        for (int c = 0; c < kKeyLoads; ++c) to.k[Tile<kDim>::key_piece(key_row + c * kKeyRows, tid % kPieces)] = keys[c];
+    auto put_values = [&](Tile<kDim> &to, auto &values, int left) {
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             const int at = quad + r * kQuads;
@@ -181,13 +182,17 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
     };
     auto store = [&](auto set, int left) {
         if constexpr (kEight) {
-            u32x4 keys[kKeyLoads];
             uint32_t values[kRounds][4][kWords];
 #pragma unroll
             for (int c = 0; c < kKeyLoads; ++c) {
                 const float scale = scale_of(key_scale[set][c]);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) keys[c][w] = values_of(key[set][c][w / 2], scale, w % 2);
+                for (int piece = 0; piece < kKeyCodes / 8; ++piece) {
+                    u32x4 x;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) x[w] = values_of(key[set][c][2 * piece + w / 2], scale, w % 2);
+                    buffer[set].k[Tile<kDim>::key_piece(key_row + c * kKeyRows, tid % kKeyThreads * (kKeyCodes / 8) + piece)] = x;
+                }
             }
 #pragma unroll
             for (int r = 0; r < kRounds; ++r)
@@ -197,18 +202,46 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
 #pragma unroll
                     for (int w = 0; w < kWords; ++w) values[r][j][w] = values_of(value[set][r][j][w / 2], scale, w % 2);
                 }
-            put(buffer[set], keys, values, left);
+            put_values(buffer[set], values, left);
         } else {
-            put(buffer[set], key[set], value[set], left);
+            // (put_values written out: handed its registers as an argument the kernels of BF16 spill 12 more of them with four waves, 9 with head_dim 256)
+            Tile<kDim> &to = buffer[set];
+#pragma unroll
+            for (int c = 0; c < kKeyLoads; ++c) to.k[Tile<kDim>::key_piece(key_row + c * kKeyRows, tid % kPieces)] = key[set][c];
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) {
+                const int at = quad + r * kQuads;
+                if (left < kKeys) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int w = 0; w < kWords; ++w) value[set][r][j][w] = 4 * at + j < left ? value[set][r][j][w] : 0u;
+                }
+#pragma unroll
+                for (int m = 0; m < 2 * kWords; ++m) {
+                    const uint32_t select = (m & 1) != 0 ? 0x07060302u : 0x05040100u;
+                    *to.value_quad(tid % kQuadThreads * (2 * kWords) + m, at) = u32x2{__builtin_amdgcn_perm(value[set][r][1][m / 2], value[set][r][0][m / 2], select),
+                                                                                      __builtin_amdgcn_perm(value[set][r][3][m / 2], value[set][r][2][m / 2], select)};
+                }
+            }
         }
     };
-    // new tokens, which are BF16 whatever the cache is
-    u32x4 new_key[kKeyLoads];
-    uint32_t new_value[kRounds][4][kWords];
+    // new tokens, which are BF16 whatever the cache is: in the registers of a tile, or in some of their own
+    u32x4 own_key[kEight ? kNewLoads : 1];
+    uint32_t own_value[kEight ? kRounds : 1][4][kWords];
+    auto &new_key = [&]() -> auto & {
+        if constexpr (kEight) return own_key;
+        else return key[0];
+    }();
+    auto &new_value = [&]() -> auto & {
+        if constexpr (kEight) return own_value;
+        else return value[0];
+    }();
+    const int new_row = tid / kPieces;
     auto load_new = [&](int start) {
 #pragma unroll
-        for (int c = 0; c < kKeyLoads; ++c)
-            new_key[c] = *reinterpret_cast<const u32x4 *>(a.k + b * a.k_batch + std::min(start + key_row + c * kKeyRows, drafted - 1) * a.k_token + h * a.k_head +
+        for (int c = 0; c < kNewLoads; ++c)
+            new_key[c] = *reinterpret_cast<const u32x4 *>(a.k + b * a.k_batch + std::min(start + new_row + c * kNewRows, drafted - 1) * a.k_token + h * a.k_head +
                                                           tid % kPieces * 16);
 #pragma unroll
         for (int r = 0; r < kRounds; ++r)
@@ -361,7 +394,13 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
                     new_value[r][j][w] = finite_part(new_value[r][j][w]);
                 }
         if (!fine) not_finite = start;
-        put(buffer[0], new_key, new_value, here);
+        if constexpr (kEight) {
+#pragma unroll
+        for (int c = 0; c < kNewLoads; ++c) buffer[0].k[Tile<kDim>::key_piece(new_row + c * kNewRows, tid % kPieces)] = new_key[c];
+        put_values(buffer[0], new_value, here);
+        } else {
+            store(even, here);
+        }
         __syncthreads();
         uint64_t sees = 0ull;
         if (t < count) {
@@ -452,5 +491,6 @@ void launch(const ArgsOf<kEight> &a, int waves, uint32_t workgroups, hipStream_t
 
 void attend_wide(const AttendArgs &a, int waves, uint32_t workgroups, hipStream_t st) { launch<false>(a, waves, workgroups, st); }
 void attend_wide(const QuantAttendArgs &a, int waves, uint32_t workgroups, hipStream_t st) { launch<true>(a, waves, workgroups, st); }
+
 
 }  // namespace fgmp
