@@ -401,6 +401,65 @@ __global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(
         for (int m = 0; m < kPer; ++m) st[r].o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
+    auto new_tokens = [&] {
+        // (the first of them to the wave behind the one that had the last tile of the range)
+        for (int tile = empty ? draft_tiles : (wave + kWaves - (end - split * per) % kWaves) % kWaves; tile < draft_tiles; tile += kWaves) {
+            const int start = tile * kKeys, last = drafted - 1 - start;
+#pragma unroll
+            for (int sub = 0; sub < kSubs; ++sub) {
+                const char *const key = a.k + b * a.k_batch + (start + std::min(16 * sub + i, last)) * a.k_token + h * a.k_head;
+                if constexpr (kEight) kt[sub].load_by_64(key + 32 * g);
+                else kt[sub].load(key + 16 * g);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    vt.load(4 * sub + j, a.v + b * a.v_batch + (start + std::min(16 * sub + 4 * g + j, last)) * a.v_token + h * a.v_head + i * kPer * kSize);
+            }
+#pragma unroll
+            for (int j = 0; j < kLaneKeys; ++j)
+                if (16 * (j / 4) + 4 * g + j % 4 > last) vt.clear(j);
+            const bool finite = __all(vt.all_finite());
+            if (!finite) vt.clear_non_finite();
+            bf16x8 columns[kPer];
+            if constexpr (!kF32) {
+#pragma unroll
+                for (int m = 0; m < kPer; ++m) columns[m] = vt.column(m);
+            }
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                // bit j: the lane's row sees new token start + j
+                uint32_t sees = 0u;
+                if (token[r] >= 0) {
+                    if (a.tree != nullptr) {
+                        const uint64_t word = a.tree[((int64_t)b * a.tokens + token[r]) * a.words + (start >> 6)];
+                        sees = (uint32_t)(word >> (start & 63));
+                    } else {
+                        const int upto = token[r] - start;
+                        sees = upto >= 31 ? 0xFFFFFFFFu : upto < 0 ? 0u : (2u << upto) - 1u;
+                    }
+                    if (last < 31) sees &= (2u << last) - 1u;
+                }
+                f32x4 s[kSubs];
+#pragma unroll
+                for (int sub = 0; sub < kSubs; ++sub) {
+                    s[sub] = scores<kF32, kDim>(kt[sub], q[r]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if ((sees >> (16 * sub + 4 * g + j) & 1u) == 0u) s[sub][j] = -INFINITY;
+                }
+                Weights<kF32, kDim> w;
+                weigh<kF32, kDim>(st[r], s, w, a.c2);
+                add_values<kF32, kDim>(st[r], w, vt, columns);
+                if (!finite)
+                    add_non_finite<kF32, kDim>(st[r], s, sees, a.v + b * a.v_batch + start * a.v_token + h * a.v_head, a.v_token,
+                                               std::min(kKeys, last + 1), a.c2);
+            }
+        }
+    };
+    // (over a short cache in 8 bits they come first: their loads and the first tile's, which has registers of its own, are waited for together.  8 x 8 heads of 1024 slots 14.8 ->
+    // 13.6 us; with head_dim 64, and with four waves over 2048 and 4096 slots, it is 0.2 to 1 slower)
+    constexpr bool kNewFirst = kEight && kWaves == kManyWaves && kDim == 128;
+    if constexpr (kNewFirst) new_tokens();
+
     for (int tile = begin; tile < end; tile += kWaves) {
         const int next = tile + kWaves, left = n - tile * kKeys;
         if (next < end) locate(next);
@@ -457,58 +516,7 @@ __global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(
             for (int r = 0; r < kRows; ++r) add_values<kF32, kDim>(st[r], w[r], vt, columns);
         }
     }
-    // (the first of them to the wave behind the one that had the last tile of the range)
-    for (int tile = empty ? draft_tiles : (wave + kWaves - (end - split * per) % kWaves) % kWaves; tile < draft_tiles; tile += kWaves) {
-        const int start = tile * kKeys, last = drafted - 1 - start;
-#pragma unroll
-        for (int sub = 0; sub < kSubs; ++sub) {
-            const char *const key = a.k + b * a.k_batch + (start + std::min(16 * sub + i, last)) * a.k_token + h * a.k_head;
-            if constexpr (kEight) kt[sub].load_by_64(key + 32 * g);
-            else kt[sub].load(key + 16 * g);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                vt.load(4 * sub + j, a.v + b * a.v_batch + (start + std::min(16 * sub + 4 * g + j, last)) * a.v_token + h * a.v_head + i * kPer * kSize);
-        }
-#pragma unroll
-        for (int j = 0; j < kLaneKeys; ++j)
-            if (16 * (j / 4) + 4 * g + j % 4 > last) vt.clear(j);
-        const bool finite = __all(vt.all_finite());
-        if (!finite) vt.clear_non_finite();
-        bf16x8 columns[kPer];
-        if constexpr (!kF32) {
-#pragma unroll
-            for (int m = 0; m < kPer; ++m) columns[m] = vt.column(m);
-        }
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            // bit j: the lane's row sees new token start + j
-            uint32_t sees = 0u;
-            if (token[r] >= 0) {
-                if (a.tree != nullptr) {
-                    const uint64_t word = a.tree[((int64_t)b * a.tokens + token[r]) * a.words + (start >> 6)];
-                    sees = (uint32_t)(word >> (start & 63));
-                } else {
-                    const int upto = token[r] - start;
-                    sees = upto >= 31 ? 0xFFFFFFFFu : upto < 0 ? 0u : (2u << upto) - 1u;
-                }
-                if (last < 31) sees &= (2u << last) - 1u;
-            }
-            f32x4 s[kSubs];
-#pragma unroll
-            for (int sub = 0; sub < kSubs; ++sub) {
-                s[sub] = scores<kF32, kDim>(kt[sub], q[r]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if ((sees >> (16 * sub + 4 * g + j) & 1u) == 0u) s[sub][j] = -INFINITY;
-            }
-            Weights<kF32, kDim> w;
-            weigh<kF32, kDim>(st[r], s, w, a.c2);
-            add_values<kF32, kDim>(st[r], w, vt, columns);
-            if (!finite)
-                add_non_finite<kF32, kDim>(st[r], s, sees, a.v + b * a.v_batch + start * a.v_token + h * a.v_head, a.v_token,
-                                           std::min(kKeys, last + 1), a.c2);
-        }
-    }
+    if constexpr (!kNewFirst) new_tokens();
 
     // join the waves: every one holds all rows over keys of its own
 #pragma unroll
