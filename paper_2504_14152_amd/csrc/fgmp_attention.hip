@@ -810,7 +810,9 @@ AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t h
         // evens out their ends over long sequences and is paid for by joining over short ones.  2 x 8 heads of 65537 slots at 256 / 512 / 1024 / 2048:
         // BF16 63 / 63 / 56 / 58 us with head_dim 64, 110 / 105 / 105 / 107 with 128, 184 / 181 / 184 / 205 with 256; 4 x 8 of 16000: 27 / 31 / 28 / 29,
         // 56 / 58 / 57 / 57, 94 / 100 / 104 / 125.  Two, 2 x 8 of 65537: 62 / 68 / 63 / 71, 114 / 112 / 116 / 129; FP32 130 / 109 / 122 / 127, 201 / 204 / 217 / 257.
-        want = p.row_groups == 1 ? 1024 : 512;
+        // Over 8 bits, whose ranges are read in half the time, as many as the chip holds: 2 x 8 heads of 131071 slots at 512 / 1024: 110 / 113 us, of 65537 63 / 68, one sequence's
+        // 8 of 32000 21.7 / 30.5, 32 of 4096 19.5 / 22.6, 32 x 8 of up to 4000 55 / 54; 256 with head_dim 256: 2 of 30000 21.2 / 32.0.
+        want = p.row_groups != 1 ? 512 : !eight ? 1024 : head_dim == 256 ? 256 : 512;
     }
     const int64_t whole = batch * heads * p.row_blocks, least = (int64_t)p.tile_keys * p.min_tiles;
     p.splits = std::max<int64_t>(1, std::min((max_length + least - 1) / least, (want + whole - 1) / whole));
