@@ -44,14 +44,14 @@ __device__ __forceinline__ float element(const char *row, int64_t i)
     else return (float)reinterpret_cast<const __bf16 *>(row)[i];
 }
 
-// (partial sums cross XCDs: accesses of agent scope, which every XCD sees once they are complete)
+// (partial sums cross XCDs: system-coherent accesses that bypass the per-XCD L2)
 __device__ __forceinline__ void store_sum(double *to, double x)
 {
-    __hip_atomic_store(reinterpret_cast<unsigned long long *>(to), __builtin_bit_cast(unsigned long long, x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(reinterpret_cast<unsigned long long *>(to), __builtin_bit_cast(unsigned long long, x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
 }
 __device__ __forceinline__ double load_sum(double *from)
 {
-    return __builtin_bit_cast(double, __hip_atomic_load(reinterpret_cast<unsigned long long *>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    return __builtin_bit_cast(double, __hip_atomic_load(reinterpret_cast<unsigned long long *>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM));
 }
 
 template <int kControl, int kRowMask>

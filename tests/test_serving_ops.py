@@ -317,7 +317,17 @@ def test_a_scale_at_the_top_of_the_range():
 
 # ---- attention over 8 bits ----
 
-@pytest.mark.parametrize("dtype,D,H,G,T,lens,page,tree,counts", [c for c in layer.ATTEND if c[0] == BF16] + [(BF16, 64, 20, 1, 2, [1000, 16], 64, False, None)])
+LONGER = [
+    (BF16, 64, 20, 1, 2, [1000, 16], 64, False, None),
+    (BF16, 128, 8, 2, 3, [3000, 0, 1500, 33], 64, True, [3, 2, 0, 1]),
+    (BF16, 64, 4, 4, 1, [2500, 1], 0, False, None),
+    (BF16, 256, 4, 2, 2, [2300, 129], 16, True, None),
+    (BF16, 128, 16, 1, 2, [2100, 64], 48, False, [2, 1]),
+    (BF16, 128, 8, 8, 1, [700] * 9, 32, False, [1, 0, 1, 1, 1, 1, 1, 0, 1]),
+]
+
+
+@pytest.mark.parametrize("dtype,D,H,G,T,lens,page,tree,counts", [c for c in layer.ATTEND if c[0] == BF16] + LONGER)
 def test_attention_over_8_bits_against_its_formula(dtype, D, H, G, T, lens, page, tree, counts):
     _say("attention8", D, H, G, T, lens, page, tree, counts)
     g = _gen(D + T + H + len(lens))
@@ -397,6 +407,40 @@ def test_hidden_tokens_reach_no_row_over_8_bits(H, G, D, bad):
     kb[0, 9] = bad
     out, lse = fgmp.tree_attention(q, kb, vb, made.cache, tree=words)
     assert torch.equal(out[0, others], plain[0, others]) and torch.equal(lse[0, others], plain_lse[0, others])
+
+
+@pytest.mark.parametrize("H,G,D,T,n", [(4, 2, 64, 1, 200), (4, 2, 128, 3, 200), (4, 2, 128, 1, 3000), (40, 2, 128, 3, 200), (4, 2, 256, 2, 200), (12, 2, 64, 9, 500)])
+def test_a_code_that_is_no_number_reaches_what_the_formula_says(H, G, D, T, n):
+    """NaN in a key: nothing but NaN for its head.  NaN in a value: in that element alone."""
+    g = _gen(14)
+    made = Made8(g, [n], G, D, 0)
+    q = _randn(g, 1, T, H, D, dtype=BF16)
+    plain, plain_lse = fgmp.tree_attention(q, None, None, made.cache)
+    made.v[0, n - 2, 1, 5] = 0x7F
+    out, lse = fgmp.tree_attention(q, None, None, made.cache)
+    per = H // G
+    bad = torch.zeros(1, T, H, D, dtype=torch.bool, device=DEV)
+    bad[:, :, per:, 5] = True
+    assert torch.equal(torch.isnan(out), bad) and torch.equal(out[~bad], plain[~bad]) and torch.equal(lse, plain_lse)
+    made.k[0, 3, 0, 1] = 0xFF
+    out, lse = fgmp.tree_attention(q, None, None, made.cache)
+    assert bool(torch.isnan(out[:, :, :per]).all()) and bool(torch.isnan(lse[:, :, :per]).all())
+    assert torch.equal(lse[:, :, per:], plain_lse[:, :, per:])
+
+
+def test_rotations_past_32_bits():
+    """Vectors more than 4 GiB behind their pointers, read and written."""
+    g = _gen(9)
+    step = 9 << 27
+    wide = torch.empty(3 * step, dtype=F32, device=DEV).as_strided((1, 3, 2, 64), (3 * step, step, 64, 1))
+    q = _randn(g, 1, 3, 2, 64)
+    wide.copy_(q)
+    f = (10000.0 ** (-torch.arange(32, device=DEV) / 32)).float()
+    want, _, _ = fgmp.rotate_heads(q, positions=_i32([[7, 8, 9]]), inv_freq=f, dtype=F32)
+    got, _, _ = fgmp.rotate_heads(wide, positions=_i32([[7, 8, 9]]), inv_freq=f, dtype=F32)
+    assert torch.equal(got, want)
+    fgmp.rotate_heads(q, positions=_i32([[7, 8, 9]]), inv_freq=f, q_out=wide)
+    assert torch.equal(wide, want)
 
 
 def test_offsets_of_8_bits_past_32_bits():
