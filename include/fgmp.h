@@ -500,7 +500,7 @@ fgmp_status_t fgmp_rotate_heads(const fgmp_heads_t *q, const fgmp_heads_t *k, co
  *   parents    nullable (a chain: t - 1); batch x tokens: the parent of each, before it; entry 0 is not read.  A token whose parent is not before it
  *              is never reached
  *   counts     nullable (tokens); per sequence, 0 .. tokens: tokens from counts[b] on are not looked at
- *   uniforms   batch x tokens numbers in 0 <= u < 1, FP32
+ *   uniforms   batch x tokens numbers in 0 <= u < 1, FP32 (outside of 0 .. 1: taken as the nearest of both, NaN as 0)
  *   rows       batch x tokens: 0 and the kept tokens, in order, then -1: what fgmp_cache_append takes as rows and, with `accepted`, as counts
  *   accepted   per sequence: how many those are (token 0 is one of them); 0 where counts[b] is
  *   next       per sequence: the token behind; -1 where counts[b] is 0 or the row has no probability above 0.  Where nothing is left of w (by

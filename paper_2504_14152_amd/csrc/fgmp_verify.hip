@@ -45,6 +45,19 @@ __device__ __forceinline__ float element(const char *row, int64_t i)
     else return (float)reinterpret_cast<const __bf16 *>(row)[i];
 }
 
+// (NaN: the smaller one of the others.  One instruction, where fmaxf takes another to quiet a NaN)
+__device__ __forceinline__ float at_least_zero(float x) { return __builtin_amdgcn_fmed3f(x, 0.0f, INFINITY); }
+
+// A probability: NaN and what is negative count as nothing.
+template <bool kF32>
+__device__ __forceinline__ float probability(const char *row, int64_t i)
+{
+    return at_least_zero(element<kF32>(row, i));
+}
+
+// A random number; outside of 0 .. 1 the nearest to it.
+__device__ __forceinline__ float within_one(float u) { return __builtin_amdgcn_fmed3f(u, 0.0f, 1.0f); }
+
 // (partial sums cross XCDs: system-coherent accesses that bypass the per-XCD L2)
 __device__ __forceinline__ void store_sum(double *to, double x)
 {
@@ -102,8 +115,8 @@ template <bool kF32>
 __device__ __forceinline__ bool look_up(const VerifyArgs &a, int b, int t, int32_t token, int32_t parent, float *p, float *q)
 {
     const bool there = t > 0 && (uint32_t)token < (uint32_t)a.vocab && (uint32_t)parent < (uint32_t)t;
-    *p = there ? element<kF32>(a.target + b * a.target_batch + parent * a.target_row, token) : 0.0f;
-    *q = there && a.draft != nullptr ? element<kF32>(a.draft + b * a.draft_batch + parent * a.draft_row, token) : 1.0f;
+    *p = there ? probability<kF32>(a.target + b * a.target_batch + parent * a.target_row, token) : 0.0f;
+    *q = there && a.draft != nullptr ? probability<kF32>(a.draft + b * a.draft_batch + parent * a.draft_row, token) : 1.0f;
     return there;
 }
 
@@ -116,11 +129,12 @@ __device__ __forceinline__ Walk walk_of_few(const VerifyArgs &a, int b)
     Walk w = {};
     w.token = t < a.n ? a.tokens[at] : -1;
     const int32_t up = a.parents != nullptr ? t < a.n ? a.parents[at] : -1 : t - 1;
-    const float u = t < a.n ? a.uniforms[at] : 0.0f;
+    const float u_read = t < a.n ? a.uniforms[at] : 0.0f;
     w.count = count = count < 0 ? 0 : count > a.n ? a.n : count;
     if (count == 0) return w;
     float p, q;
     const bool there = look_up<kF32>(a, b, t < count ? t : 0, w.token, up, &p, &q);
+    const float u = within_one(u_read);
     if (a.parents == nullptr) {
         // up to the first one that is refused
         const uint64_t fails = __ballot(t > 0 && t < count && !((double)u * (double)q < (double)p));
@@ -149,7 +163,7 @@ __device__ __forceinline__ Walk walk_of_few(const VerifyArgs &a, int b)
                 w.kept_lanes |= 1ull << child;
             } else {
                 w.refused_lanes |= 1ull << child;
-                left -= p_child > 0.0f ? (double)p_child : 0.0;
+                left -= (double)p_child;
             }
         }
         if (!kept) break;
@@ -167,7 +181,7 @@ __device__ __forceinline__ Walk walk_of_many(const VerifyArgs &a, int b, ManyTok
     __syncthreads();
     for (int t = threadIdx.x; t < count; t += kThreads) {
         const int32_t token = a.tokens[at + t], parent = a.parents != nullptr ? a.parents[at + t] : t - 1;
-        const float u = a.uniforms[at + t];
+        const float u = within_one(a.uniforms[at + t]);
         float p, q;
         const bool there = look_up<kF32>(a, b, t, token, parent, &p, &q);
         if (a.parents == nullptr && t > 0 && !((double)u * (double)q < (double)p)) atomicMin(&s.first_refused, t);
@@ -194,7 +208,7 @@ __device__ __forceinline__ Walk walk_of_many(const VerifyArgs &a, int b, ManyTok
                     s.last = t, s.refused = 0, left = 1.0;
                 } else {
                     s.refused_token[s.refused++] = s.token[t];
-                    left -= p > 0.0 ? p : 0.0;
+                    left -= p;
                 }
             }
         }
@@ -222,6 +236,8 @@ __device__ __forceinline__ void weights_of(const VerifyArgs &a, int b, int segme
         const char *draft = a.draft + b * a.draft_batch + walk.last * a.draft_row;
 #pragma unroll
         for (int r = 0; r < kRows; ++r) q[r] = element<kF32>(draft, full ? first + 64 * r : std::min(first + 64 * r, a.vocab - 1));
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) q[r] = at_least_zero(q[r]);
     } else {
 #pragma unroll
         for (int r = 0; r < kRows; ++r) q[r] = 0.0f;
@@ -239,11 +255,13 @@ __device__ __forceinline__ void weights_of(const VerifyArgs &a, int b, int segme
             }
         }
     }
+    // (what is not above 0, or NaN, is nothing)
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-        const double x = (double)p[r] - (double)q[r];
-        w[r] = x > 0.0 && (full || first + 64 * r < a.vocab) ? x : 0.0;   // (NaN counts as nothing)
-    }
+    for (int r = 0; r < kRows; ++r) w[r] = fmax((double)p[r] - (double)q[r], 0.0);
+    if (full) return;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+        if (first + 64 * r >= a.vocab) w[r] = 0.0;
 }
 
 template <bool kF32, bool kFew, int kRows, typename Tokens>
@@ -271,8 +289,7 @@ __device__ __forceinline__ int32_t pick(const VerifyArgs &a, int b, const Walk &
     for (int i = first + kHeld; i < end; ++i) mine += sum_at(i);
     const double incl = wave_scan(mine), total = of_lane(incl, 63);
     if (!(total > 0.0)) return -1;
-    const double u = u0 > 0.0f ? u0 < 1.0f ? (double)u0 : 1.0 : 0.0;   // (outside of 0 .. 1: nearest to it)
-    const double wanted = u * total;
+    const double wanted = (double)within_one(u0) * total;
     // The first lane up to which more than that is summed up, and of its segments the first one; where rounding leaves none, the last that has anything.
     const uint64_t over = __ballot(mine > 0.0 && incl > wanted), some = __ballot(mine > 0.0);
     const int owner = over != 0ull ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);

@@ -476,8 +476,8 @@ def test_offsets_of_8_bits_past_32_bits():
 
 def _verified(target, tokens, u, draft, parents, counts):
     """By the definition, in 64 bits on the CPU: rows, accepted, and the token behind with the sums around its draw."""
-    target, tokens, u = target.double().cpu(), tokens.tolist(), u.double().cpu()
-    draft = None if draft is None else draft.double().cpu()
+    target, tokens, u = target.double().cpu().nan_to_num(0.0).clamp(min=0), tokens.tolist(), u.double().cpu().nan_to_num(0.0).clamp(0, 1)
+    draft = None if draft is None else draft.double().cpu().nan_to_num(0.0).clamp(min=0)
     B, N, V = target.shape
     rows, accepted, behind = [], [], []
     for b in range(B):
@@ -584,6 +584,57 @@ def test_a_workspace_serves_one_verification_after_another():
         got = fgmp.verify_drafts(target, tokens.int().to(DEV), u.to(DEV), workspace=ws)
         assert [x.tolist() for x in got] == list(_verified(target, tokens, u, None, None, [6] * B))
         assert not bool(ws[:fgmp.WORKSPACE_CONTROL_BYTES].any())
+
+
+@pytest.mark.parametrize("N", [1, 2, 63, 64, 65, 200])
+@pytest.mark.parametrize("kind", ["chain", "given", "path", "children"])
+def test_everything_is_kept_or_refused(N, kind):
+    """Around the most tokens that a wave walks over by itself.  Of one token with N - 1 children all but the last are refused."""
+    _say("verify all", N, kind)
+    g = _gen(N)
+    V = 777
+    target = _distributions(g, 2, N, V)
+    tokens = target.roll(1, 1).argmax(-1)
+    u = torch.zeros(2, N)
+    draft = parents = None
+    if kind == "chain":
+        draft = _distributions(g, 2, N - 1, V).to(DEV)
+    elif kind == "path":
+        parents = (torch.arange(N) - 1).expand(2, N)
+    elif kind == "children":
+        parents = torch.zeros(2, N, dtype=torch.int64)
+        tokens = torch.arange(N).expand(2, N)
+        target[:, 0] = torch.rand(2, V, generator=g) + 0.5
+        target[:, 0] /= target[:, 0].sum(-1, keepdim=True)
+        u[:] = 1.0 - 2.0 ** -24
+        u[:, -1] = 0.0
+    u[:, 0] = 0.6
+    got = fgmp.verify_drafts(target.to(DEV), tokens.int().to(DEV), u.to(DEV), draft=draft, parents=None if parents is None else parents.int().contiguous().to(DEV))
+    assert [x.tolist() for x in got] == list(_verified(target, tokens, u, draft, parents, [N] * 2))
+    assert got[1].tolist() == [min(N, 2) if kind == "children" else N] * 2
+
+
+@pytest.mark.parametrize("N", [4, 70])
+@pytest.mark.parametrize("bad", [math.nan, -2.0])
+def test_what_is_no_probability_counts_as_zero(N, bad):
+    """In the drafted distributions too: such a token is kept where the target has it, never where the target has 0, and takes nothing from w."""
+    g = _gen(int(N))
+    B, V = 64, 1500
+    target, draft = _distributions(g, B, N, V), _distributions(g, B, N - 1, V)
+    target[torch.rand(B, N, V, generator=g) < 0.3] = bad
+    target[torch.rand(B, N, V, generator=g) < 0.3] = 0.0
+    draft[torch.rand(B, N - 1, V, generator=g) < 0.5] = bad
+    tokens = torch.randint(0, V, (B, N), generator=g)
+    tokens[::7, 1] = -1
+    tokens[3::7, 1] = V
+    u = torch.rand(B, N, generator=g) * 1.4 - 0.2
+    u[5::9] = math.nan
+    for given in (None, draft):
+        got = fgmp.verify_drafts(target.to(DEV), tokens.int().to(DEV), u.to(DEV), draft=None if given is None else given.to(DEV))
+        assert [x.tolist() for x in got] == list(_verified(target, tokens, u, given, None, [N] * B)), given is None
+        parents = torch.zeros(B, N, dtype=torch.int64)
+    got = fgmp.verify_drafts(target.to(DEV), tokens.int().to(DEV), u.to(DEV), parents=parents.int().to(DEV))
+    assert [x.tolist() for x in got] == list(_verified(target, tokens, u, None, parents, [N] * B))
 
 
 def test_rows_of_which_nothing_is_left():
