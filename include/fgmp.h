@@ -410,7 +410,7 @@ fgmp_status_t fgmp_cache_evict(const fgmp_cache_t *cache, const float *weights, 
  * nearest codes, ties to even; what is not finite becomes NaN.  Values are exact in FP32 and in BF16 (an element that rounds up to 2^128 becomes infinite).
  *   codes      a cache as above of dtype FGMP_E4M3: elements of one byte, page_size a multiple of 16 with or without a page table
  *   k_scales, v_scales   one byte e + 127 for each: of row r of page p and head h at p * scale_page_stride + h * scale_head_stride + r.
- *              Pointers and strides are multiples of 16 bytes
+ *              Pointers and strides are multiples of 16 bytes.  An append writes 27 to 247; 0 and 255 are no scales
  * fgmp_attention_weights and fgmp_cache_evict take no such cache.
  */
 typedef struct {

@@ -268,10 +268,23 @@ def _ptr(t) -> int | None:
     return None if t is None else t.data_ptr()
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+@functools.lru_cache(maxsize=None)
+def _several_devices() -> bool:
+    return torch.cuda.device_count() > 1
+
+
 def _require_cuda(*tensors) -> None:
     for t in tensors:
         if t is not None and not t.is_cuda:
             raise FgmpError("all tensors must live on the GPU")
+    if _several_devices():
+        here = _current_device()
+        for t in tensors:
+            if t is not None and t.get_device() != here:
+                raise FgmpError(f"all tensors must live on the current device, {here}")
 
 
 @dataclass

@@ -324,3 +324,29 @@ def test_a_tensor_says_the_same_either_way():
         assert n == t.dim() and tuple(sizes[:n]) == t.shape and tuple(strides[:n]) == t.stride() and kind.value == types.get(t.dtype, -1)
         assert (data.value or 0) == t.data_ptr()
     assert look(base[None], 4, sizes, strides, ctypes.byref(kind), ctypes.byref(data)) == -1
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    monkeypatch.setattr(fgmp, "_stream", lambda: 0)
+    monkeypatch.setattr(fgmp, "_several_devices", lambda: True)
+    monkeypatch.setattr(fgmp, "_current_device", lambda: 1)
+
+    class On(torch.Tensor):
+        is_cuda = True
+        device_of = 1
+
+        def get_device(self):
+            return self.device_of
+
+    def on(device, t):
+        t = t.as_subclass(On)
+        t.device_of = device
+        return t
+
+    here, there = (on(d, torch.zeros(2, 3, 4, 64)) for d in (1, 0))
+    with pytest.raises(fgmp.FgmpError, match="current device, 1"):
+        fgmp.rotate_heads(here, there)
+    with pytest.raises(fgmp.FgmpError, match="^k: "):        # (of this device: looked at further)
+        fgmp.rotate_heads(here, on(1, torch.zeros(2, 3, 4, 32)))
+    with pytest.raises(fgmp.FgmpError, match="current device, 1"):
+        fgmp.verify_drafts(here[0], on(0, torch.zeros(3, 4, dtype=torch.int32)), here[0, :, :, 0])
