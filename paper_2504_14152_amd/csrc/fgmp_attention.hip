@@ -583,29 +583,98 @@ __global__ void __launch_bounds__(64 * kWaves, kRows > 1 ? 2 : 1) attend_kernel(
     }
 }
 
+// Over rows of 16 lanes, the same in all of them: neighbours, then pairs, quads, eights.
+template <typename Op>
+__device__ __forceinline__ float over_16(float x, Op op)
+{
+    auto step = [&](auto control) {
+        x = op(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(control)::value, 0xF, 0xF, true)));
+    };
+    step(std::integral_constant<int, 0xB1>());    // lane ^ 1
+    step(std::integral_constant<int, 0x4E>());    // lane ^ 2
+    step(std::integral_constant<int, 0x141>());   // 7 - lane of eight
+    step(std::integral_constant<int, 0x140>());   // 15 - lane of a row
+    return x;
+}
+
 template <int kN>
 struct FloatsOf {
     typedef float type __attribute__((ext_vector_type(kN)));
 };
 
-// Joins the ranges of keys.  kWavesPerRow waves to a row: a lane holds the maximum and sum of one range (of every 64), and each wave adds
-// up every kWavesPerRow-th range.  One wave does for up to 16 ranges (12800 rows of 4 ranges, head_dim 128: 9.5 us, 20.5 with four waves, of
-// which three have hardly anything to do), four for more (64 rows of 64 ranges: 7 us, 36 with one).
-template <bool kF32, int kDim, int kWavesPerRow>
-__global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int64_t rows)
+template <bool kF32, int kN>
+__device__ __forceinline__ void store_joined(char *to, int lane, typename FloatsOf<kN>::type o)
 {
-    constexpr int kPer = kDim / 64, kRowsHere = 4 / kWavesPerRow;
-    using part = typename FloatsOf<kPer>::type;
-    __shared__ part sums[kWavesPerRow][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = wave % kWavesPerRow;
-    const int64_t at = (int64_t)blockIdx.x * kRowsHere + wave / kWavesPerRow;
-    if (kWavesPerRow == 1 && at >= rows) return;
-    const int head = (int)((uint32_t)at % (uint32_t)a.q_heads);
-    const uint32_t bt = (uint32_t)at / (uint32_t)a.q_heads;
+#pragma unroll
+    for (int e = 0; e < kN; ++e) {
+        if constexpr (kF32) reinterpret_cast<float *>(to)[lane * kN + e] = o[e];
+        else reinterpret_cast<__bf16 *>(to)[lane * kN + e] = (__bf16)o[e];
+    }
+}
+
+// Joins up to kFewRanges ranges of keys: kDim / 4 lanes have a row, 16 of them each the maximum and sum of a range.  What the first four ranges hold is
+// asked for before it is known how many are in use: one trip to memory for all
+// (12800 rows of 4 ranges, head_dim 128: 7.4 us, 9.2 with a wave to a row that asks for ranges in use; four waves to a row had hardly anything to do, 20).
+constexpr int kFewRanges = 16;
+template <bool kF32, int kDim>
+__global__ void __launch_bounds__(256) join_few_kernel(AttendArgs a, uint32_t rows)
+{
+    constexpr int kLanes = kDim / 4, kRowsHere = 256 / kLanes, kAtATime = 4;
+    const int lane = threadIdx.x % kLanes, range = threadIdx.x % kFewRanges, first_lane = (threadIdx.x & 63) / kLanes * kLanes;
+    const uint32_t place = blockIdx.x * kRowsHere + threadIdx.x / kLanes, at = std::min(place, rows - 1u);
+    const f32x4 *po = reinterpret_cast<const f32x4 *>(a.part_o + (int64_t)at * a.splits * kDim) + lane;
+    f32x4 x[kAtATime];
+    auto load = [&](int from) {
+#pragma unroll
+        for (int j = 0; j < kAtATime; ++j) x[j] = po[std::min(from + j, a.splits - 1) * kLanes];
+    };
+    load(0);
+    const float2 ml = reinterpret_cast<const float2 *>(a.part_ml)[(int64_t)at * a.splits + std::min(range, a.splits - 1)];
+    const int head = (int)(at % (uint32_t)a.q_heads);
+    const uint32_t bt = at / (uint32_t)a.q_heads;
     const int t = (int)(bt % (uint32_t)a.tokens), b = (int)(bt / (uint32_t)a.tokens);
     const int used = t < a.count(b) ? a.ranges(a.c.length(b)) : 0;
-    const float *ml = a.part_ml + at * a.splits * 2;
-    const part *po = reinterpret_cast<const part *>(a.part_o + at * a.splits * kDim) + lane;
+    const float m = range < used ? ml.x : -INFINITY, most = over_16(m, [](float p, float q) { return fmaxf(p, q); });
+    const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - most) * a.c2);
+    const float l = over_16(range < used ? ml.y * f : 0.0f, [](float p, float q) { return p + q; });
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int first = 0; first < a.splits; first += kAtATime) {
+        if (first > 0) load(first);
+#pragma unroll
+        for (int j = 0; j < kAtATime; ++j) {
+            const float factor = __shfl(f, first_lane + first + j);
+            if (first + j < used) o += x[j] * factor;
+        }
+    }
+    if (place >= rows) return;
+    o *= inverse_sum(l);
+    store_joined<kF32, 4>(a.out + b * a.o_batch + t * a.o_token + head * a.o_head, lane, o);
+    if (lane == 0) a.lse[at] = logsumexp(most, l, a.c2);
+}
+
+// Joins more of them, a workgroup to a row: a lane holds the maximum and sum of one range (of every 64), and each wave adds up every fourth
+// range, the first of them asked for before it is known how many are in use (128 rows of 32 ranges: 4.8 us, 5.2 asked for later; 64 rows of 64 took one wave a
+// row 36 us, four 7).
+template <bool kF32, int kDim>
+__global__ void __launch_bounds__(256) join_many_kernel(AttendArgs a)
+{
+    constexpr int kPer = kDim / 64, kWavesPerRow = 4, kAtATime = 8;
+    using part = typename FloatsOf<kPer>::type;
+    __shared__ part sums[kWavesPerRow][64];
+    const int lane = threadIdx.x & 63, share = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t at = blockIdx.x;
+    const part *po = reinterpret_cast<const part *>(a.part_o + (int64_t)at * a.splits * kDim) + lane;
+    part x[kAtATime];
+    auto load = [&](int from) {
+#pragma unroll
+        for (int j = 0; j < kAtATime; ++j) x[j] = po[std::min(from + kWavesPerRow * j, a.splits - 1) * 64];
+    };
+    load(share);
+    const float *ml = a.part_ml + (int64_t)at * a.splits * 2;
+    const int head = (int)(at % (uint32_t)a.q_heads);
+    const uint32_t bt = at / (uint32_t)a.q_heads;
+    const int t = (int)(bt % (uint32_t)a.tokens), b = (int)(bt / (uint32_t)a.tokens);
+    const int used = t < a.count(b) ? a.ranges(a.c.length(b)) : 0;
     float most = -INFINITY;
     for (int s = lane; s < used; s += 64) most = fmaxf(most, ml[2 * s]);
 #pragma unroll
@@ -620,12 +689,10 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int64_t rows)
             l += ml[2 * (start + lane) + 1] * f;
         }
         const int here = std::min(64, used - start);
-        for (int first = share; first < here; first += 4 * kWavesPerRow) {
-            part x[4];
+        for (int first = share; first < here; first += kAtATime * kWavesPerRow) {
+            if (start + first > share) load(start + first);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = po[(start + std::min(first + kWavesPerRow * j, here - 1)) * 64];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < kAtATime; ++j) {
                 const float factor = __shfl(f, first + kWavesPerRow * j);
                 if (first + kWavesPerRow * j < here) o += x[j] * factor;
             }
@@ -633,20 +700,12 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int64_t rows)
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
-    if constexpr (kWavesPerRow > 1) {
-        sums[wave][lane] = o;
-        __syncthreads();
-        if (wave != 0) return;
-        o = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
-    }
+    sums[share][lane] = o;
+    __syncthreads();
+    if (share != 0) return;
+    o = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
     o *= inverse_sum(l);
-    char *to = a.out + b * a.o_batch + t * a.o_token + head * a.o_head;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const float x = o[e];
-        if constexpr (kF32) reinterpret_cast<float *>(to)[lane * kPer + e] = x;
-        else reinterpret_cast<__bf16 *>(to)[lane * kPer + e] = (__bf16)x;
-    }
+    store_joined<kF32, kPer>(a.out + b * a.o_batch + t * a.o_token + head * a.o_head, lane, o);
     if (lane == 0) a.lse[at] = logsumexp(most, l, a.c2);
 }
 
@@ -844,8 +903,8 @@ void attend_launch(const ArgsOf<kEight> &a, const AttendPlan &p, hipStream_t st)
         if (p.row_groups == 2) attend_kernel<kF32, kDim, 2, kEight><<<grid, 64 * kFewWaves, 0, st>>>(a);
     }
     const int64_t rows = (int64_t)a.c.batch * a.tokens * a.q_heads;
-    if (p.splits > 16) join_kernel<kF32, kDim, 4><<<dim3((unsigned)rows), 256, 0, st>>>(a, rows);
-    else if (p.splits > 1) join_kernel<kF32, kDim, 1><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(a, rows);
+    if (p.splits > kFewRanges) join_many_kernel<kF32, kDim><<<dim3((unsigned)rows), 256, 0, st>>>(a);
+    else if (p.splits > 1) join_few_kernel<kF32, kDim><<<dim3((unsigned)((rows + 1024 / kDim - 1) / (1024 / kDim))), 256, 0, st>>>(a, (uint32_t)rows);
 }
 
 }  // namespace
