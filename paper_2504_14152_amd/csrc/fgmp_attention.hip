@@ -876,9 +876,9 @@ AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t h
     const int64_t whole = batch * heads * p.row_blocks, least = (int64_t)p.tile_keys * p.min_tiles;
     p.splits = std::max<int64_t>(1, std::min((max_length + least - 1) / least, (want + whole - 1) / whole));
     p.waves = kFewWaves;
-    // A short cache in 8 bits is not cut: twice the waves, and no launch to join.  One sequence's 32 heads of 517 / 1024 / 2048 slots, cut / not: 11.8 / 9.8, 13.1 / 12.9,
-    // 16.8 / 21.7 us; 8 x 8 heads 13.2 / 10.4, 16.5 / 14.7, 25.1 / 21.9, of 4096 29.9 / 36.4 (head_dim 256 has no registers for so many waves)
-    if (eight && p.row_groups == 1 && head_dim != 256 && p.splits > 1 && max_length <= (whole >= 64 ? 2048 : 1024)) p.splits = 1, p.waves = kManyWaves;
+    // A short cache in 8 bits is not cut: twice the waves, and no launch to join.  One sequence's 32 heads of 517 / 1024 / 2048 slots, cut / not: 10.8 / 9.6, 11.9 / 12.2,
+    // 16.2 / 21.7 us; 8 x 8 heads 12.3 / 9.9, 15.7 / 13.6, 18.6 / 20.0; 16 x 8 13.7 / 10.8, 17.4 / 13.6, 21.6 / 20.0 (head_dim 256 has no registers for so many waves)
+    if (eight && p.row_groups == 1 && head_dim != 256 && p.splits > 1 && max_length <= (whole >= 128 ? 2048 : 1024)) p.splits = 1, p.waves = kManyWaves;
     p.units = batch * heads * p.splits;
     p.workgroups = (p.units + 7) / 8 * 8 * p.row_blocks;
     return p;
