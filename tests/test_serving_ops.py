@@ -256,6 +256,43 @@ def test_append_quantizes(source, G, D, page, T, lens, counts, outside):
     assert lengths.tolist() == [n + c for n, c in zip(lens, use)]
 
 
+@pytest.mark.parametrize("source", [BF16, F32])
+@pytest.mark.parametrize("G,D,page,T,lens,counts", [(1, 64, 64, 9001, [0, 77], None), (1, 128, 0, 4097, [3, 0, 50], [4097, 0, 4000]), (3, 256, 48, 811, [47, 1], [811, 805]),
+                                                    (8, 128, 16, 300, [5, 0, 16, 31], [300, 299, 1, 300]), (5, 64, 32, 1300, [31, 0, 1], [1300, 1299, 3]),
+                                                    (20, 128, 64, 130, [0, 9], None)])
+def test_append_of_many_tokens_quantizes(source, G, D, page, T, lens, counts):
+    """As many as workgroups have several of: rows in any order, some that are none, a page that is none, more tokens than slots."""
+    _say("append8 many", source, G, D, page, T, lens, counts)
+    g = _gen(T + G)
+    B = len(lens)
+    use = [T] * B if counts is None else counts
+    made = Made8(g, lens, G, D, page, room=T - 20)          # (the first sequence's slots may end before its tokens)
+    k, v = _vectors(g, B, T, G, D, dtype=source), _vectors(g, B, T, 2 * G, D, dtype=source)[:, :, ::2]
+    rows = torch.stack([torch.randperm(T, generator=g) for _ in range(B)]).int()
+    rows[0, 1], rows[0, 17], rows[-1, 0] = T, -3, T - 1
+    cache, lost = made.cache, -1
+    if page:
+        lost = max(1, lens[0] // page + 1)
+        table = made.table.clone()
+        table[0, lost] = 1 << 30                            # what falls there is dropped
+        cache = fgmp.QuantCache(made.k.view(E4M3), made.v.view(E4M3), made.ks, made.vs, _i32(lens), table.to(DEV))
+    want = [x.cpu() for x in (made.k, made.v, made.ks, made.vs)]
+    lengths = fgmp.cache_append(k, v, cache, rows=rows.to(DEV), counts=None if counts is None else _i32(counts))
+    for x, c, s in ((k, want[0], want[2]), (v, want[1], want[3])):
+        code, scale = _quantized(x)
+        for b in range(B):
+            i = torch.arange(min(use[b], made.slots - lens[b]))
+            r, slot = rows[b, i].long(), lens[b] + i
+            entry = slot // page if page else torch.zeros_like(slot)
+            fine = (r >= 0) & (r < T) & ((entry != lost) if b == 0 else True)
+            r, slot, entry = r[fine], slot[fine], entry[fine]
+            at = made.table[b, entry].long() if page else torch.full_like(slot, b)
+            c[at, slot % made.size], s[at, :, slot % made.size] = code[b, r], scale[b, r]
+    assert _is_code(made.k, want[0]) and _is_code(made.v, want[1])
+    assert torch.equal(made.ks.cpu(), want[2]) and torch.equal(made.vs.cpu(), want[3])
+    assert lengths.tolist() == [min(n + c, made.slots) for n, c in zip(lens, use)]
+
+
 def test_append_into_8_bits_drops_what_has_no_slot_and_no_page():
     g = _gen(10)
     made = Made8(g, [30, 32], 1, 64, 16)       # 32 slots each
@@ -274,7 +311,9 @@ def test_append_into_8_bits_drops_what_has_no_slot_and_no_page():
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("G,D,page,lens,first,tokens,outside", [(2, 64, 16, [40, 3, 0], 0, 48, False), (8, 128, 0, [700], 333, 100, True), (3, 256, 48, [100, 47], 17, 1, False),
-                                                               (1, 128, 64, [130], 130, 2, False), (16, 128, 32, [95, 64, 65], 31, 40, True)])
+                                                               (1, 128, 64, [130], 130, 2, False), (16, 128, 32, [95, 64, 65], 31, 40, True),
+                                                               (1, 128, 64, [9000, 8003], 5, 8995, False), (3, 128, 48, [4000, 3999, 0], 17, 3983, True), (8, 64, 0, [3001], 0, 3001, False),
+                                                               (5, 256, 16, [2000, 17], 1, 1999, False), (8, 128, 64, [2100], 3, 2090, False)])
 def test_reading_back(dtype, G, D, page, lens, first, tokens, outside):
     _say("read8", dtype, G, D, page, lens, first, tokens)
     g = _gen(D + first)
