@@ -852,7 +852,11 @@ AttendPlan attend_plan(int64_t batch, int64_t tokens, int64_t q_heads, int64_t h
     AttendPlan p = {};
     const int64_t groups = (tokens * (q_heads / heads) + 15) / 16;
     int64_t want;   // workgroups asked for, by making ranges
-    if (!f32 && groups > (head_dim == 256 ? 1 : 2)) {
+    // The kernel for many rows begins with three groups (two with head_dim 256).  Over a short cache in 8 bits it is not worth its stages below five: one sequence of 1000
+    // slots, 8 heads, three groups, with it / without: 13.3 / 12.1 us with head_dim 64, 18.0 / 15.9 with 128, 16 of 1500 23.9 / 22.3 and 35.1 / 32.4, 3 of 4000 24.0 / 23.2
+    // and 33.8 / 33.4, 2 of 30000 32.5 / 36.4 and 53.0 / 58.7; 4 heads of 256: one of 1000 24.7 / 17.7, 3 of 4000 49.5 / 39.4, 16 of 1500 42.7 / 51.6, 2 of 30000 85 / 127.
+    const bool few = eight && groups <= 4 && (head_dim == 256 ? max_length <= 4096 && batch * heads * groups < 128 : max_length <= 2048);
+    if (!f32 && !few && groups > (head_dim == 256 ? 1 : 2)) {
         p.waves_of_rows = groups <= 8 || head_dim == 256 ? 4 : 8;
         p.row_blocks = (groups + 2 * p.waves_of_rows - 1) / (2 * p.waves_of_rows);
         p.tile_keys = wide_keys((int)head_dim);

@@ -363,6 +363,14 @@ LONGER = [
     (BF16, 256, 4, 2, 2, [2300, 129], 16, True, None),
     (BF16, 128, 16, 1, 2, [2100, 64], 48, False, [2, 1]),
     (BF16, 128, 8, 8, 1, [700] * 9, 32, False, [1, 0, 1, 1, 1, 1, 1, 0, 1]),
+    # 33 to 64 rows (17 to 64 of head_dim 256), over caches on either side of what the kernel for many rows begins with
+    (BF16, 128, 8, 1, 6, [2500, 300], 64, True, None),
+    (BF16, 128, 8, 1, 7, [1000, 3, 0], 64, True, [7, 6, 2]),
+    (BF16, 64, 8, 1, 8, [4100], 0, False, None),
+    (BF16, 64, 16, 2, 5, [2047, 33], 16, True, [5, 3]),
+    (BF16, 256, 8, 1, 4, [4200, 5], 16, True, None),
+    (BF16, 256, 16, 2, 7, [90, 17] * 8 + [0], 16, False, None),
+    (BF16, 256, 16, 2, 8, [1700, 0, 64], 64, True, [8, 1, 5]),
 ]
 
 
