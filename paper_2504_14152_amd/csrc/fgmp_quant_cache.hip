@@ -4,7 +4,7 @@
 // power of two loses nothing against a scale of its own making: the format's steps are relative to an element, not to the vector, and x 2^-e
 // and code 2^e are exact, the latter in BF16 too.  Both calls are bounded by memory, as long as a vector, eight elements to each of kLanes lanes, takes few
 // instructions (the card's own conversions, with their scales) and enough vectors are under way: 16387 tokens of 32 heads of 128, FP32, are appended in 114 us,
-// 5.9 TB/s; 65536 of 8 heads, BF16, in 44 us, 4.5 TB/s; 4 sequences of up to 16381 slots of 32 heads are read back as BF16 in 255 us, 5.1 TB/s, two thirds of it written.
+// 5.9 TB/s; 65536 of 8 heads, BF16, in 44 us, 4.5 TB/s; 4 sequences of up to 16381 slots of 32 heads are read back as BF16 in 254 us, 5.1 TB/s, two thirds of it written.
 #include <algorithm>
 #include <type_traits>
 

@@ -7,7 +7,7 @@
 // A few dependent round trips to memory bound it (tokens, their probabilities, the row), then the row's bytes: waves add up segments of 64 kRows elements
 // each, a wave of the workgroup that is its sequence's last finds the segment, and in it the element.  Up to 64 tokens each wave does the
 // walk in its own lanes.  Sums are of 64 bits: in 32, those over a vocabulary are off by more than many a token's probability.
-// A tree of 25 tokens over 32000: 7.6 us; 32 chains of 8 over 151937, two rows each: 13 us, of which 5 pass before the 39 MB are asked for.
+// A tree of 25 tokens over 32000: 7.1 us; 32 chains of 8 over 151937, two rows each: 13 us, of which 5 pass before the 39 MB are asked for.
 #include <algorithm>
 #include <type_traits>
 
