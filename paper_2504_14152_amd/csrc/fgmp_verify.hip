@@ -20,8 +20,11 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMaxTokens = 1024, kFewTokens = 64;
 // Rows of 64 elements in a segment.  Short ones where the chip holds all their waves at a time, long ones else: one sequence of 32000, 4 / 8 / 16 rows: 7.5 / 7.5 / 10.4
-// us; 32 sequences of 2 x 151937: 19.9 / 13.7 / 13.1.
-constexpr int kShortRows = 8, kLongRows = 16, kWavesAtATime = 4096;
+// us; 64 of 50000, 8 / 16: 11.9 / 14.8; 32 of 2 x 151937, 4 / 8 / 16 / 32: 19.9 / 13.7 / 13.1 / 15.
+constexpr int kShortRows = 8, kLongRows = 16, kWavesAtATime = 8192;
+// Workgroups at most: about as many as the chip holds, whose waves then have several segments but walk once (64 sequences of 262144 at 768 / 1280 / 2048 / 8192: 21.7 /
+// 21.2 / 25.0 / 28.3 us).
+constexpr int64_t kMostWorkgroups = 1280;
 constexpr int kHeld = 8;           // sums of segments that a lane keeps in registers
 constexpr int64_t kMaxVocab = (int64_t)1 << 24, kMaxBatch = 16384;
 
@@ -479,7 +482,7 @@ fgmp_status_t fgmp_verify_drafts(const void *target, fgmp_dtype_t dt, int64_t ta
     a.counters = static_cast<uint32_t *>(workspace);
     a.sums = reinterpret_cast<double *>(static_cast<char *>(workspace) + kWsCtrlRegion);
     const int64_t most = (a.segments + kWaves - 1) / kWaves;
-    a.workgroups = (uint32_t)std::min<int64_t>(most, std::max<int64_t>(2, 8192 / batch));
+    a.workgroups = (uint32_t)std::min<int64_t>(most, std::max<int64_t>(2, kMostWorkgroups / batch));
     const dim3 grid((unsigned)(batch * a.workgroups));
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (dt == FGMP_F32) launch<true>(a, row_count, grid, st);

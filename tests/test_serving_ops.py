@@ -581,6 +581,8 @@ VERIFY = [
     (1, 300, 700, "tree", F32, None),
     (1, 2, 300001, "chain", F32, None),
     (1100, 3, 100, "chain", F32, None),
+    (600, 2, 9000, "chain", BF16, None),        # (more segments than a sequence's workgroups have waves)
+    (300, 3, 20001, "given", F32, None),
 ]
 
 
