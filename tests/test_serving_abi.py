@@ -77,7 +77,7 @@ def test_attention_over_8_bits_refuses():
 def test_append_and_read_refuse():
     assert _append(out=None) == INVALID and _append(out=AT) == INVALID and _append(dt=2) == INVALID and _append(tokens=0) == INVALID
     assert _append(accepted=3) == SHAPE and _append(accepted=0) == INVALID and _append(k=_heads(None)) == INVALID and _append(v=_heads(AT + 8)) == ALIGN
-    assert _append(cache=_quant(batch=MANY), tokens=257, accepted=257) == UNSUPPORTED     # (2^32 threads and more)
+    assert _append(cache=_quant(batch=MANY), tokens=1 << 20, accepted=1 << 20) == UNSUPPORTED     # (2^32 threads and more)
     assert _read(first=-1) == INVALID and _read(tokens=0) == INVALID and _read(dt=2) == INVALID and _read(first=255) == SHAPE and _read(tokens=257) == SHAPE
     assert _read(first=(1 << 63) - 1, tokens=2) == SHAPE and _read(first=0, tokens=(1 << 63) - 1) == SHAPE
     assert _read(k=_heads(None)) == INVALID and _read(v=_heads(AT + 8)) == ALIGN and _read(k=_heads(strides=(1024, 0, 128))) == SHAPE
