@@ -17,7 +17,7 @@
 typedef int (*fused_fn)(const void *, int, int64_t, int64_t, int64_t, const float *, float, float, const void *, int64_t, float *,
                         int64_t, void *, size_t, void *);
 
-static PyObject *s_is_cuda, *s_shape, *s_dtype, *s_data_ptr, *s_stride, *s_numel, *s_K, *s_rows, *s_buf, *zero;
+static PyObject *s_is_cuda, *s_shape, *s_dtype, *s_data_ptr, *s_stride, *s_numel, *s_K, *s_rows, *s_buf, *s_get_device, *zero;
 
 /* a plain GPU tensor's dimensions, sizes, strides, type and address without asking its attributes (fgmp_tensors.cpp); NULL: there is no such way */
 typedef int (*look_fn)(PyObject *, int, int64_t *, int64_t *, int *, void **);
@@ -29,6 +29,18 @@ static PyObject *look_into_tensors(PyObject *self, PyObject *address)
     void *const p = PyLong_AsVoidPtr(address);
     if (PyErr_Occurred()) return NULL;
     look = (look_fn)p;
+    Py_RETURN_NONE;
+}
+
+/* what says which device is the current one; NULL: there is one device, and no tensor is asked for its own */
+static PyObject *current_device_of;
+
+static PyObject *current_device(PyObject *self, PyObject *callable)
+{
+    (void)self;
+    PyObject *const before = current_device_of;
+    current_device_of = callable == Py_None ? NULL : Py_NewRef(callable);
+    Py_XDECREF(before);
     Py_RETURN_NONE;
 }
 
@@ -84,6 +96,24 @@ static int64_t elements(PyObject *tensor, int *bad)
     return *bad ? 0 : integer(PyObject_VectorcallMethod(s_numel, args, 1, NULL), bad);
 }
 
+/* The current device, asked for once in a call (*here < 0: not yet). */
+static int64_t the_device(int64_t *here, int *bad)
+{
+    if (*here < 0 && !*bad) *here = integer(PyObject_CallObject(current_device_of, NULL), bad);
+    return *here;
+}
+
+/* whether a tensor is on the GPU, and on the current one where there are several */
+static int on_the_gpu(PyObject *tensor, int64_t *here)
+{
+    if (!is_true(tensor, s_is_cuda)) return 0;
+    if (current_device_of == NULL) return 1;
+    int bad = 0;
+    PyObject *const args[1] = {tensor};
+    const int64_t its = integer(PyObject_VectorcallMethod(s_get_device, args, 1, NULL), &bad);
+    return its == the_device(here, &bad) && !bad;
+}
+
 static double number(PyObject *o, int *bad)
 {
     if (*bad) return 0.0;
@@ -106,10 +136,10 @@ static PyObject *quant_gemm_fused(PyObject *self, PyObject *const *a, Py_ssize_t
     }
     PyObject *const X = a[3], *const fisher = a[4], *const pW = a[7], *const out = a[8], *const workspace = a[9];
     int bad = 0;
-    int64_t M = 0, K = 0;
+    int64_t M = 0, K = 0, here = -1;
     PyObject *v = NULL;
 
-    if (!is_true(X, s_is_cuda) || !is_true(fisher, s_is_cuda)) goto general;
+    if (!on_the_gpu(X, &here) || !on_the_gpu(fisher, &here)) goto general;
     v = PyObject_GetAttr(X, s_shape);
     if (v == NULL || !PyTuple_Check(v) || PyTuple_GET_SIZE(v) != 2) goto general;
     Py_INCREF(PyTuple_GET_ITEM(v, 0));
@@ -126,7 +156,7 @@ static PyObject *quant_gemm_fused(PyObject *self, PyObject *const *a, Py_ssize_t
     const int64_t N = attribute(pW, s_rows, &bad);
     if (bad) goto general;
     v = PyObject_GetAttr(pW, s_buf);
-    if (v == NULL) goto general;
+    if (v == NULL || !on_the_gpu(v, &here) || !on_the_gpu(out, &here) || !on_the_gpu(workspace, &here)) goto general;
     const void *const w = pointer(v, &bad);
     Py_CLEAR(v);
     const void *const x = pointer(X, &bad);
@@ -160,6 +190,7 @@ enum { F32, BF16, I32, I64, U8, N_TYPES };
 typedef struct {
     int64_t size[26];          /* by letter; -1: not known yet */
     PyObject *const *types;    /* torch.float32, .bfloat16, .int32, .int64, .uint8 */
+    int64_t here;              /* the current device; -1: not asked for yet */
     int bad;
 } call_t;
 
@@ -168,6 +199,7 @@ static int64_t *letter(call_t *c, char x) { return &c->size[x - 'A']; }
 static void begin(call_t *c, PyObject *types)
 {
     for (int i = 0; i < 26; ++i) c->size[i] = -1;
+    c->here = -1;
     c->bad = !PyTuple_Check(types) || PyTuple_GET_SIZE(types) != N_TYPES;
     c->types = c->bad ? NULL : &PyTuple_GET_ITEM(types, 0);
 }
@@ -203,7 +235,7 @@ static void *tensor(call_t *c, PyObject *t, const char *letters, int types, int 
     if (seen >= 0) {
         if (seen != n || k < 0 || !(types >> k & 1)) return NULL;
     } else {
-        if (!is_true(t, s_is_cuda)) return NULL;
+        if (!on_the_gpu(t, &c->here)) return NULL;
         PyObject *v = PyObject_GetAttr(t, s_dtype);
         while (k < N_TYPES && (!(types >> k & 1) || v != c->types[k])) ++k;
         Py_XDECREF(v);
@@ -236,12 +268,17 @@ static fgmp_heads_t heads(call_t *c, PyObject *t, const char *letters, int types
     return h;
 }
 
-/* A cache's handle: (address of its description, B, G, D, S, dtype): batch, heads, head_dim, slots */
+/* A cache's handle: (address of its description, B, G, D, S, dtype, device): batch, heads, head_dim, slots; the device may be left out where there is one */
 static const fgmp_cache_t *cache_of(call_t *c, PyObject *handle, int *types)
 {
-    if (c->bad || !PyTuple_Check(handle) || PyTuple_GET_SIZE(handle) != 6) {
+    if (c->bad || !PyTuple_Check(handle) || PyTuple_GET_SIZE(handle) < 6 || PyTuple_GET_SIZE(handle) > 7) {
         c->bad = 1;
         return NULL;
+    }
+    if (current_device_of != NULL) {
+        const int64_t its = PyTuple_GET_SIZE(handle) == 7 ? integer(Py_NewRef(PyTuple_GET_ITEM(handle, 6)), &c->bad) : -1;
+        if (its != the_device(&c->here, &c->bad)) c->bad = 1;
+        if (c->bad) return NULL;
     }
     for (int i = 0; i < 4; ++i) {
         *letter(c, "BGDS"[i]) = PyLong_AsLongLong(PyTuple_GET_ITEM(handle, i + 1));
@@ -521,13 +558,15 @@ static PyObject *verify_drafts(PyObject *self, PyObject *const *a, Py_ssize_t n)
 static PyMethodDef methods[] = {METHOD(quant_gemm_fused), METHOD(tree_attention), METHOD(attention_weights), METHOD(cache_append), METHOD(cache_evict),
                                 METHOD(block_norm), {"quant_cache_attention", (PyCFunction)(void (*)(void))tree_attention, METH_FASTCALL, NULL},
                                 METHOD(quant_cache_append), METHOD(quant_cache_read), METHOD(rotate_heads), METHOD(verify_drafts),
-                                {"look_into_tensors", look_into_tensors, METH_O, NULL}, {NULL, NULL, 0, NULL}};
+                                {"look_into_tensors", look_into_tensors, METH_O, NULL}, {"current_device", current_device, METH_O, NULL},
+                                {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fgmp_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__fgmp_call(void)
 {
     struct { PyObject **at; const char *name; } const names[] = {{&s_is_cuda, "is_cuda"}, {&s_shape, "shape"}, {&s_dtype, "dtype"},
-        {&s_data_ptr, "data_ptr"}, {&s_stride, "stride"}, {&s_numel, "numel"}, {&s_K, "K"}, {&s_rows, "rows"}, {&s_buf, "buf"}};
+        {&s_data_ptr, "data_ptr"}, {&s_stride, "stride"}, {&s_numel, "numel"}, {&s_K, "K"}, {&s_rows, "rows"}, {&s_buf, "buf"},
+        {&s_get_device, "get_device"}};
     for (size_t i = 0; i < sizeof names / sizeof names[0]; ++i)
         if ((*names[i].at = PyUnicode_InternFromString(names[i].name)) == NULL) return NULL;
     if ((zero = PyLong_FromLong(0)) == NULL) return NULL;

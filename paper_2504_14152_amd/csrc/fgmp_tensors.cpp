@@ -10,16 +10,16 @@ extern "C" {
 
 const char *fgmp_tensors_torch(void) { return TORCH_VERSION; }
 
-/* Dimensions of a plain tensor on the current GPU (not of a subclass, which may answer for itself), up to `most`, with its sizes, strides, address and type: 0
- * float32, 1 bfloat16, 2 int32, 3 int64, 4 uint8, -1 another.  -1: nothing is said about `o`; more
- * than `most`: it does not fit. */
+/* Dimensions of a plain tensor on the GPU (not of a subclass, which may answer for itself), up to `most`, with its sizes, strides, address and type: 0
+ * float32, 1 bfloat16, 2 int32, 3 int64, 4 uint8, -1 another.  most + 1: it is on another device than the current one.  -1: nothing is said about `o`, one of more dimensions
+ * among others. */
 int fgmp_tensors_look(PyObject *o, int most, int64_t *sizes, int64_t *strides, int *type, void **data)
 {
     if (!THPVariable_CheckExact(o)) return -1;
     try {
         const at::Tensor &t = THPVariable_Unpack(o);
         if (!t.is_cuda() || t.layout() != at::kStrided || t.dim() > most) return -1;
-        /* (on another device it is for the general path to refuse: the attributes do not say which device is the current one) */
+        /* (on another device than the current one it does not fit; the general path says so) */
         static const c10::impl::DeviceGuardImplInterface *const gpu = c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA);
         static const bool several = gpu->deviceCount() > 1;   /* (asking for the current one is 0.05 us) */
         if (several && t.device().index() != gpu->getDevice().index()) return most + 1;

@@ -95,6 +95,7 @@ def _load_call():
         loader.exec_module(module)
     except (ImportError, OSError, RuntimeError):
         return None
+    module.current_device(_current_device if _several_devices() else None)
     _load_tensors(module)
     return module
 
@@ -277,6 +278,7 @@ def _several_devices() -> bool:
 
 
 def _require_cuda(*tensors) -> None:
+    """Calls run on the current device's current stream: refuses a tensor that is not there, and so do the extension module's ways."""
     for t in tensors:
         if t is not None and not t.is_cuda:
             raise FgmpError("all tensors must live on the GPU")
@@ -293,6 +295,10 @@ class Packed:
     buf: torch.Tensor   # uint8
     rows: int
     K: int
+
+
+def _buf(p: Packed | None) -> torch.Tensor | None:
+    return None if p is None else p.buf
 
 
 def version() -> str:
@@ -337,7 +343,7 @@ EPILOGUE_NONE, EPILOGUE_SILU_GATE, EPILOGUE_ONE_LAUNCH = 0, 1, 0x100   # fgmp_ep
 
 def quantize_weights(W: torch.Tensor, fisher: torch.Tensor, threshold: float, tensor_scale: float,
                      want_scores: bool = False, out: Packed | None = None, score_mode: str | None = None):
-    _require_cuda(W, fisher)
+    _require_cuda(W, fisher, _buf(out))
     N, K = W.shape
     ldf = 0 if fisher.dim() == 1 else fisher.stride(0)
     out = out or _alloc_packed(N, K, W.device)
@@ -357,7 +363,7 @@ def quantize_weights(W: torch.Tensor, fisher: torch.Tensor, threshold: float, te
 def quantize_weights_clip(W: torch.Tensor, fisher: torch.Tensor, threshold: float, tensor_scale: float,
                           want_scores: bool = False, out: Packed | None = None):
     """quantize_weights with the block scales chosen by sensitivity-weighted clipping (Eq. 11)."""
-    _require_cuda(W, fisher)
+    _require_cuda(W, fisher, _buf(out))
     N, K = W.shape
     ldf = 0 if fisher.dim() == 1 else fisher.stride(0)
     out = out or _alloc_packed(N, K, W.device)
@@ -372,7 +378,7 @@ def quantize_weights_clip(W: torch.Tensor, fisher: torch.Tensor, threshold: floa
 
 def quantize_activations(X: torch.Tensor, fisher_k: torch.Tensor, threshold: float, tensor_scale: float,
                          want_scores: bool = False, out: Packed | None = None, score_mode: str | None = None):
-    _require_cuda(X, fisher_k)
+    _require_cuda(X, fisher_k, _buf(out))
     M, K = X.shape
     out = out or _alloc_packed(M, K, X.device)
     scores = torch.empty((M, K // 16), dtype=torch.float32, device=X.device) if want_scores else None
@@ -391,6 +397,7 @@ def quantize_activations(X: torch.Tensor, fisher_k: torch.Tensor, threshold: flo
 def gemm(pX: Packed, pW: Packed, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     if pX.K != pW.K:
         raise FgmpError("K mismatch")
+    _require_cuda(pX.buf, pW.buf, out, workspace)
     M, N, K = pX.rows, pW.rows, pX.K
     Y = out if out is not None else torch.empty((M, N), dtype=torch.float32, device=pX.buf.device)
     if workspace is None:
@@ -414,7 +421,7 @@ def quant_gemm_fused(X: torch.Tensor, fisher_k: torch.Tensor, threshold: float, 
             if rc != 0:
                 _check(rc, "fgmp_quant_gemm_fused")
             return out
-    _require_cuda(X, fisher_k)
+    _require_cuda(X, fisher_k, pW.buf, out, workspace)
     M, K = X.shape
     if K != pW.K:
         raise FgmpError("K mismatch")
@@ -441,7 +448,7 @@ def quant_gemm_fused_static_scratch(X: torch.Tensor, fisher_k: torch.Tensor, thr
                                     pW: Packed, out: torch.Tensor) -> torch.Tensor:
     """quant_gemm_fused without a workspace: the library's static scratch array serves (small products
     only).  `out` is required: the binding allocates nothing either."""
-    _require_cuda(X, fisher_k, out)
+    _require_cuda(X, fisher_k, pW.buf, out)
     M, K = X.shape
     if K != pW.K:
         raise FgmpError("K mismatch")
@@ -458,7 +465,7 @@ def quant_gemm_fused_packed_out(X: torch.Tensor, fisher_k: torch.Tensor, thresho
                                 workspace: torch.Tensor | None = None, epilogue: int | None = None):
     """Fused step whose results are quantized and packed (a packed M x N activation tensor; with
     epilogue=EPILOGUE_SILU_GATE the gated activation of the 32 + 32 row groups of W, M x N/2)."""
-    _require_cuda(X, fisher_k, fisher_n)
+    _require_cuda(X, fisher_k, pW.buf, fisher_n, _buf(out), workspace)
     M, K = X.shape
     if K != pW.K:
         raise FgmpError("K mismatch")
@@ -488,6 +495,7 @@ def quant_gemm_fused_packed_out(X: torch.Tensor, fisher_k: torch.Tensor, thresho
 
 def unpack_canonical(p: Packed):
     """(codes [rows,K] u8, scales [rows,K/16] u8, mask [rows,K/16] u8) on the device."""
+    _require_cuda(p.buf)
     dev = p.buf.device
     codes = torch.empty((p.rows, p.K), dtype=torch.uint8, device=dev)
     scales = torch.empty((p.rows, p.K // 16), dtype=torch.uint8, device=dev)
@@ -499,6 +507,7 @@ def unpack_canonical(p: Packed):
 
 def dequantize_f16(p: Packed, out: torch.Tensor | None = None) -> torch.Tensor:
     """Dense FP16 values (without the tensor scale), zero-padded to [rows_out, ld]."""
+    _require_cuda(p.buf, out)
     ld = -(-p.K // 128) * 128
     if out is None:
         out = torch.empty((-(-p.rows // 8) * 8, ld), dtype=torch.float16, device=p.buf.device)
@@ -510,7 +519,7 @@ def dequantize_f16(p: Packed, out: torch.Tensor | None = None) -> torch.Tensor:
 def quantize_dequantize_f16(X: torch.Tensor, fisher_k: torch.Tensor, threshold: float, tensor_scale: float,
                             out: torch.Tensor | None = None) -> torch.Tensor:
     """FP16 values of the codes the quantizer selects (without the tensor scale), [rows_out, ld]."""
-    _require_cuda(X, fisher_k)
+    _require_cuda(X, fisher_k, out)
     M, K = X.shape
     if out is None:
         out = torch.empty((-(-M // 8) * 8, -(-K // 128) * 128), dtype=torch.float16, device=X.device)
@@ -522,6 +531,7 @@ def quantize_dequantize_f16(X: torch.Tensor, fisher_k: torch.Tensor, threshold: 
 
 
 def packed_info(p: Packed) -> dict:
+    _require_cuda(p.buf)
     info = _PackedInfo()
     _check(lib().fgmp_packed_info(_ptr(p.buf), ctypes.byref(info), _stream()), "fgmp_packed_info")
     return {name: getattr(info, name) for name, _ in _PackedInfo._fields_}
@@ -538,8 +548,9 @@ def threshold_for_fraction(scores: torch.Tensor, fraction: float) -> float:
 
 def threshold_for_fraction_multi(score_tensors, fraction: float) -> float:
     """One threshold over several score tensors (a global threshold over layers, Eq. 10)."""
-    flat = [t.contiguous().view(-1) for t in score_tensors]
+    flat = list(score_tensors)
     _require_cuda(*flat)
+    flat = [t.contiguous().view(-1) for t in flat]
     n = len(flat)
     ptrs = (ctypes.c_void_p * n)(*[t.data_ptr() for t in flat])
     counts = (ctypes.c_int64 * n)(*[t.numel() for t in flat])
@@ -594,7 +605,7 @@ def selftest_time_gemm_kernel(start: "torch.cuda.Event | None", stop: "torch.cud
 
 def selftest_quantizer_traffic(X: torch.Tensor, fisher_k: torch.Tensor, out: Packed) -> None:
     """Launch the traffic model of the activation quantizer (measurement builds only; the caller times it)."""
-    _require_cuda(X, fisher_k)
+    _require_cuda(X, fisher_k, out.buf)
     M, K = X.shape
     _check(lib().fgmp_selftest_quantizer_traffic(_ptr(X), _dtype_code(X), M, K, X.stride(0), _ptr(fisher_k), _ptr(out.buf),
                                                  out.buf.numel(), _stream()), "fgmp_selftest_quantizer_traffic")
@@ -648,7 +659,7 @@ class Cache:
                                     k.stride(0), k.stride(1), k.stride(2), _ptr(page_table), 0 if page_table is None else page_table.stride(0),
                                     None)
         self._ref = ctypes.byref(self._struct)
-        self._handle = (ctypes.addressof(self._struct), self.batch, heads, dim, self.slots, k.dtype)
+        self._handle = (ctypes.addressof(self._struct), self.batch, heads, dim, self.slots, k.dtype, k.get_device() if _several_devices() else 0)
         self.lengths = lengths
 
     @property
@@ -657,7 +668,7 @@ class Cache:
 
     @lengths.setter
     def lengths(self, value: torch.Tensor) -> None:
-        _require_cuda(value)
+        _require_cuda(value, self.k)
         _check_int32(value, "lengths", (self.batch,))
         self._lengths = value
         self._struct.lengths = value.data_ptr()
@@ -690,7 +701,7 @@ class QuantCache:
                              _ptr(page_table), 0 if page_table is None else page_table.stride(0), None)
         self._struct = _QuantCacheStruct(codes, k_scales.data_ptr(), v_scales.data_ptr(), k_scales.stride(0), k_scales.stride(1))
         self._ref = ctypes.byref(self._struct)
-        self._handle = (ctypes.addressof(self._struct), self.batch, heads, dim, self.slots, torch.bfloat16)
+        self._handle = (ctypes.addressof(self._struct), self.batch, heads, dim, self.slots, torch.bfloat16, k.get_device() if _several_devices() else 0)
         self.lengths = lengths
 
     @property
@@ -699,7 +710,7 @@ class QuantCache:
 
     @lengths.setter
     def lengths(self, value: torch.Tensor) -> None:
-        _require_cuda(value)
+        _require_cuda(value, self.k)
         _check_int32(value, "lengths", (self.batch,))
         self._lengths = value
         self._struct.codes.lengths = value.data_ptr()
@@ -755,7 +766,7 @@ def tree_attention(q: torch.Tensor, k: torch.Tensor | None, v: torch.Tensor | No
     if out is not None and lse is not None and workspace is not None and scale is not None and _handed(
             entry, q, k, v, cache._handle, tree, counts, scale, max_length, out, lse, workspace):
         return out, lse
-    _require_cuda(q, k, v, tree, counts, out, lse, workspace)
+    _require_cuda(q, k, v, cache.k, tree, counts, out, lse, workspace)
     if q.dim() != 4 or (k is None) != (v is None):
         raise FgmpError("q: batch x tokens x heads x head_dim; k and v: both or neither")
     B, T, H, D = q.shape
@@ -790,7 +801,7 @@ def attention_weights(q: torch.Tensor, lse: torch.Tensor, cache: Cache, weights:
     if scale is not None and _handed("attention_weights", q, lse, cache._handle, weights, rows, counts, scale, max_length,
                                      weights if out is None else out):
         return weights if out is None else out
-    _require_cuda(q, lse, weights, rows, counts, out)
+    _require_cuda(q, lse, cache.k, weights, rows, counts, out)
     if q.dim() != 4 or q.shape[0] != cache.batch or q.shape[3] != cache.head_dim:
         raise FgmpError("q does not match the cache")
     B, T, H, D = q.shape
@@ -832,7 +843,7 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, cache: Cache | QuantCache, ro
         return _quant_append(k, v, cache, rows, counts, lengths_out)
     if lengths_out is not None and _handed("cache_append", k, v, cache._handle, rows, counts, positions, slot_positions, slot_weights, lengths_out):
         return lengths_out
-    _require_cuda(k, v, rows, counts, positions, slot_positions, slot_weights, lengths_out)
+    _require_cuda(k, v, cache.k, rows, counts, positions, slot_positions, slot_weights, lengths_out)
     if k.dim() != 4 or k.dtype != v.dtype:
         raise FgmpError("k and v: batch x tokens x heads x head_dim, of one type")
     T = k.shape[1]
@@ -855,7 +866,7 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, cache: Cache | QuantCache, ro
 def _quant_append(k, v, cache: QuantCache, rows, counts, lengths_out) -> torch.Tensor:
     if lengths_out is not None and _handed("quant_cache_append", k, v, cache._handle, rows, counts, lengths_out):
         return lengths_out
-    _require_cuda(k, v, rows, counts, lengths_out)
+    _require_cuda(k, v, cache.k, rows, counts, lengths_out)
     if k.dim() != 4 or k.dtype != v.dtype:
         raise FgmpError("k and v: batch x tokens x heads x head_dim, of one type")
     T, shape = k.shape[1], (cache.batch, k.shape[1], cache.heads, cache.head_dim)
@@ -878,7 +889,7 @@ def cache_read(cache: QuantCache, first: int = 0, tokens: int | None = None, k_o
         raise FgmpError("cache_read takes a QuantCache")
     if k_out is not None and v_out is not None and tokens is None and _handed("quant_cache_read", cache._handle, first, k_out, v_out):
         return k_out, v_out
-    _require_cuda(k_out, v_out)
+    _require_cuda(cache.k, k_out, v_out)
     given = k_out if k_out is not None else v_out
     if given is not None:
         if given.dim() != 4 or (tokens is not None and tokens != given.shape[1]):
@@ -911,7 +922,7 @@ def cache_evict(cache: Cache, weights: torch.Tensor, positions: torch.Tensor, se
     if lengths_out is not None and workspace is not None and _handed(
             "cache_evict", cache._handle, weights, positions, seen, budget, sinks, recent, weights_out, positions_out, lengths_out, workspace):
         return weights_out, positions_out, lengths_out
-    _require_cuda(weights, positions, seen, weights_out, positions_out, lengths_out, workspace)
+    _require_cuda(cache.k, weights, positions, seen, weights_out, positions_out, lengths_out, workspace)
     shape = (cache.batch, cache.heads, weights.shape[-1])
     _check_f32(weights, "weights", shape)
     _check_f32(weights_out, "weights_out", shape)
