@@ -14,6 +14,8 @@ import sys
 import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
+import torch.version
+
 from . import listing_check
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -23,9 +25,9 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "fgmp.h")
 CALL_SOURCE = os.path.join(CSRC, "fgmp_call.c")
 # what the binding hands the fused call's arguments over with; the name says for which interpreter
 CALL = os.path.join(HERE, "_fgmp_call" + sysconfig.get_config_var("EXT_SUFFIX"))
-# what that module looks into tensors with; for this interpreter and its torch
+# what that module looks into tensors with; for this interpreter and its torch, whose C++ objects are no other build's: the name has its version and commit
 TENSORS_SOURCE = os.path.join(CSRC, "fgmp_tensors.cpp")
-TENSORS = os.path.join(HERE, "_fgmp_tensors" + sysconfig.get_config_var("EXT_SUFFIX"))
+TENSORS = os.path.join(HERE, f"_fgmp_tensors.{torch.version.__version__}.{str(torch.version.git_version)[:12]}{sysconfig.get_config_var('EXT_SUFFIX')}")
 SOURCES = ["fgmp_quantize.hip", "fgmp_gemm.hip", "fgmp_gemm_skinny.hip", "fgmp_gemm_stream.hip", "fgmp_gemm_mid.hip",
            "fgmp_gemm_mixed.hip",
            "fgmp_select.hip", "fgmp_attention.hip", "fgmp_attention_wide.hip", "fgmp_cache.hip",
@@ -106,7 +108,6 @@ def build_call() -> str:
 
 def build_tensors() -> str:
     """What it looks into tensors with, for the torch that runs here."""
-    import torch
     root = os.path.dirname(torch.__file__)
     include = os.path.join(root, "include")
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
