@@ -125,13 +125,19 @@ class Layer:
         return fgmp.block_norm(x, z, pre_weight=self.norm[2], out=x, h=self.b_h[0])
 
     def accept(self, rows: torch.Tensor | None = None, counts: torch.Tensor | None = None, most: int | None = None) -> None:
-        """Keeps the tokens of the last pass that were accepted (`rows`, `counts`; all unless given; `most`: no sequence more than that)."""
+        """Keeps the tokens of the last pass that were accepted (`rows`, `counts`; all unless given; `most`: no sequence more than that).  A cache in
+        8 bits is never cut: RuntimeError, and nothing is kept, where a sequence has no room left."""
         old = self.cache.lengths
         if self.bits == 8:
+            most = self.tokens if most is None else most
+            if self.held + most > self.cache.slots:     # (that is a bound; from here on the GPU has to be asked)
+                self.held = int(old.max())
+                if int((old + (self.tokens if counts is None else counts)).max()) > self.cache.slots:
+                    raise RuntimeError(f"the cache is full: a sequence has {self.cache.slots} slots")
             self.cache.lengths = fgmp.cache_append(self.k, self.v, self.cache, rows=rows, counts=counts,
                                                    lengths_out=self.lengths[0] if old is not self.lengths[0] else self.lengths[1])
             self.seen = self.seen + (self.tokens if counts is None else counts)
-            self.held = min(self.cache.slots, self.held + (self.tokens if most is None else most))
+            self.held = min(self.cache.slots, self.held + most)
             return
         new = fgmp.cache_append(self.k, self.v, self.cache, rows=rows, counts=counts, positions=self.new_positions, slot_positions=self.positions,
                                 slot_weights=self.weights, lengths_out=self.lengths[0] if old is not self.lengths[0] else self.lengths[1])
