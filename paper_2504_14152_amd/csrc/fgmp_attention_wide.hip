@@ -396,8 +396,8 @@ __global__ void __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) attend_wide_
         if (!fine) not_finite = start;
         if constexpr (kEight) {
 #pragma unroll
-        for (int c = 0; c < kNewLoads; ++c) buffer[0].k[Tile<kDim>::key_piece(new_row + c * kNewRows, tid % kPieces)] = new_key[c];
-        put_values(buffer[0], new_value, here);
+            for (int c = 0; c < kNewLoads; ++c) buffer[0].k[Tile<kDim>::key_piece(new_row + c * kNewRows, tid % kPieces)] = new_key[c];
+            put_values(buffer[0], new_value, here);
         } else {
             store(even, here);
         }
@@ -491,6 +491,5 @@ void launch(const ArgsOf<kEight> &a, int waves, uint32_t workgroups, hipStream_t
 
 void attend_wide(const AttendArgs &a, int waves, uint32_t workgroups, hipStream_t st) { launch<false>(a, waves, workgroups, st); }
 void attend_wide(const QuantAttendArgs &a, int waves, uint32_t workgroups, hipStream_t st) { launch<true>(a, waves, workgroups, st); }
-
 
 }  // namespace fgmp

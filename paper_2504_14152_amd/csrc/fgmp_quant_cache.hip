@@ -4,7 +4,7 @@
 // power of two loses nothing against a scale of its own making: the format's steps are relative to an element, not to the vector, and x 2^-e
 // and code 2^e are exact, the latter in BF16 too.  Both calls are bounded by memory, as long as a vector, eight elements to each of kLanes lanes, takes few
 // instructions (the card's own conversions, with their scales) and enough vectors are under way: 16387 tokens of 32 heads of 128, FP32, are appended in 114 us,
-// 5.9 TB/s; 65536 of 8 heads, BF16, in 44 us, 4.5 TB/s; 4 sequences of up to 16381 slots of 32 heads are read back as BF16 in 254 us, 5.1 TB/s, two thirds of it written.
+// 5.9 TB/s; 32768 of 8 heads, BF16, in 44 us, 4.5 TB/s (65536 in 83, 4.9 TB/s); 4 sequences of up to 16381 slots of 32 heads are read back as BF16 in 254 us, 5.1 TB/s, two thirds of it written.
 #include <algorithm>
 #include <type_traits>
 
@@ -30,16 +30,14 @@ fgmp_status_t check_quant_cache(const fgmp_quant_cache_t *c, QuantCacheView *vie
 
 namespace {
 
-typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 constexpr int kThreads = 256;
-// Appended tokens go several to a workgroup where that leaves as many workgroups, but for FP32 whose tokens fill one by themselves: 65536 tokens of 8 heads of 128, BF16,
-// 54 -> 44 us, FP32 63 -> 67; 524288 of one head 213 -> 45 and 67.  Below, a call is mostly its launch either way.
+// Appended tokens go several to a workgroup where that leaves as many workgroups, but for FP32 whose tokens fill one by themselves: 32768 tokens of 8 heads of 128, BF16,
+// 54 -> 44 us, FP32 63 -> 67; 262144 of one head, BF16, 213 -> 45 (FP32 67).  Below, a call is mostly its launch either way.
 constexpr int64_t kManyWorkgroups = 256;
 
 struct HeadsAt {

@@ -7,6 +7,8 @@
 // A few dependent round trips to memory bound it (tokens, their probabilities, the row), then the row's bytes: waves add up segments of 64 kRows elements
 // each, a wave of the workgroup that is its sequence's last finds the segment, and in it the element.  Up to 64 tokens each wave does the
 // walk in its own lanes.  Sums are of 64 bits: in 32, those over a vocabulary are off by more than many a token's probability.
+// Of more than 64 tokens one thread of each workgroup walks, in LDS: a tree of 65 / 256 / 1024 over 32000: 12 / 21 / 64 us.  Tokens refused where the walk ends are gone through
+// again for each segment, and past 64 tokens for each child behind them too: 24 / 63 / 255 / 1023 refused children of one token: 26 / 58 / 1700 / 24000 us.
 // A tree of 25 tokens over 32000: 7.1 us; 32 chains of 8 over 151937, two rows each: 13 us, of which 5 pass before the 39 MB are asked for.
 #include <algorithm>
 #include <type_traits>
